@@ -195,6 +195,76 @@ int sasgd_applyUpdateNoAlloc(const float* theta_in_dev, float* theta_out_dev, fl
                              int32_t lr_mode, float alpha0, float momentum, float weight_decay, void* stream,
                              char* err, size_t err_len);
 
+/* ---- AdamW over many tensors, and the norm that bounds its gradients --------------------- */
+
+/* Both calls are context-free and allocate nothing, like applyUpdateNoAlloc: caller-owned device memory, kernels enqueued on
+ * `stream` (hipStream_t, NULL = default stream; it belongs to the current device), err / err_len an optional host buffer that
+ * receives a message when a call fails.  They may be captured into a graph.  Calls that overlap in time must not share
+ * moments or a workspace.  Pointers need the alignment of their elements only, the moments 16 bytes; where the weights, gradients
+ * and copies of a tensor are 16-, 16- (bf16: 8-) and 8-byte aligned it is moved 16 bytes a lane. */
+
+/* gradientNorm: out_dev[0] = sqrt(sum over all tensors of g^2), squares and sums in 64 bits in a fixed order; out_dev[1] = the factor
+ * that bounds the norm: 1 where max_norm is 0 or the norm is not above it, max_norm / norm beyond, NaN where the norm is not finite.
+ *   grads_dev: HOST array of `count` device pointers; numel: HOST array of their lengths (0 allowed, any pointer then);
+ *   type: SASGD_FP32 or SASGD_BF16, of all gradients; workspace_dev: SASGD_NORM_WORKSPACE bytes, 8-byte aligned, any contents.
+ * Errors: EINVAL (argument), EHIP. */
+#define SASGD_NORM_WORKSPACE 16384
+int sasgd_gradientNorm(const void* const* grads_dev, const int64_t* numel, int32_t count, int32_t type, float max_norm,
+                       float* out_dev, void* workspace_dev, void* stream, char* err, size_t err_len);
+
+enum { SASGD_MOMENTS_FP32 = 0, SASGD_MOMENTS_E4M3 = 1 };
+
+typedef struct {
+  int32_t lr_mode;       /* SASGD_LR_*: a_l = 1 / max(tau_l, 1); 1 / max(mean tau, 1); 1                        */
+  int32_t moments;       /* SASGD_MOMENTS_*                                                                     */
+  int32_t grad_type;     /* SASGD_FP32 or SASGD_BF16                                                            */
+  uint32_t seed;         /* of the roundings of E4M3 moments                                                    */
+  double alpha0, beta1, beta2, epsilon, weight_decay;
+} sasgd_adamw;
+
+typedef struct {
+  int64_t numel;         /* 0 allowed: the tensor is passed over                                                */
+  const float* theta_in; /* device float32 [numel]                                                              */
+  float* theta_out;      /* device float32 [numel]; theta_in for a step in place, else memory apart from it     */
+  uint16_t* shadow_out;  /* optional: bf16 [numel], receives theta_out rounded to nearest even                  */
+} sasgd_tensor;
+
+/* Moments of all tensors of a step, side by side: every tensor takes ceil(numel / 256) blocks of 256 elements, in the order of
+ * the tensors, so that each begins at a multiple of 256; sasgd_momentElements says how many elements that makes.  All start as
+ * zeros; what lies behind a tensor's last element is neither read into a result nor kept (E4M3: it becomes 0).
+ *   MOMENTS_FP32: m, v float32 [elements]; the scales are not read.
+ *   MOMENTS_E4M3: m and u = sqrt(v) as OCP e4m3 bytes [elements] with a float32 scale per block [elements / 256], the
+ *   block's largest magnitude / 448 (0 where that is below 1e-30).  A value is rounded up or down at random, up with the
+ *   probability of what is cut off (in 1/65536), so that its expectation is kept: v moves by a thousandth a step where two e4m3
+ *   values are a tenth apart, and would stand still if it were rounded to the nearest.  The 32 random bits of an element (upper half
+ *   m, lower half u) are mix(lo 0x9E3779B1 ^ hi 0x243F6A89 ^ mix(seed + step 0x9E3779B1)) of its place (hi, lo) in the moments,
+ *   modulo 2^32, mix(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xB7E15163, x ^= x >> 16.  A u above 0 becomes at least
+ *   the smallest e4m3 value, as it is divided by.  A gradient that is not finite makes its block's scale NaN. */
+typedef struct {
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+} sasgd_moments;
+
+int sasgd_momentElements(const int64_t* numel, int32_t count, int64_t* out_elements);
+
+/* applyAdamW: one AdamW step of `count` tensors, from c gradients each:
+ *     rate = alpha0 mean_l(a_l);   g = factor sum_l (a_l / sum a) g_l
+ *     m <- beta1 m + (1 - beta1) g;   v <- beta2 v + (1 - beta2) g^2
+ *     theta_out = theta_in (1 - rate weight_decay) - rate / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + epsilon)
+ * rate g is the sum of coef_l g_l that sumGradients defines; the step's length follows the staleness although the moments take
+ * the gradients' size out of it.  With c = 1 and staleness 0 this is AdamW at the rate alpha0.  All arithmetic is fp32, each operation
+ * rounded by itself.
+ *   grads_dev: HOST array of count c device pointers, those of tensor k at [k c .. k c + c); staleness: HOST int32 [c];
+ *   step: t >= 1; step_dev: optional device int64 that holds t instead (a captured graph reads it at every replay);
+ *   factor_dev: optional device float, gradientNorm's out_dev + 1; where it holds NaN the step is left out: the moments stay, and
+ *   theta_out / shadow_out take theta_in.
+ * Errors: EINVAL (argument), EHIP. */
+int sasgd_applyAdamW(const sasgd_adamw* rule, const sasgd_tensor* tensors, int32_t count, const void* const* grads_dev, int32_t c,
+                     const int32_t* staleness, const sasgd_moments* moments, int64_t step, const int64_t* step_dev,
+                     const float* factor_dev, void* stream, char* err, size_t err_len);
+
 /* ---- training-loop pieces around the hot path (Sections 4.1 - 4.3) ---------------------- */
 
 /* evaluate: forward pass only over the bound mini-batches of the listed learners, each on its

@@ -23,6 +23,8 @@ LR_MODES = {"per_gradient": 0, "mean_staleness": 1, "constant": 2}
 FLAG_FLAT_FC_GRADIENT = 1
 FLAG_EAGER_UPDATES = 2
 COMPUTE = {"fp32": 0, "bf16": 1}
+MOMENTS_FP32, MOMENTS_E4M3 = 0, 1
+NORM_WORKSPACE = 16384
 
 EXPORTS = [
     "sasgd_create", "sasgd_destroy", "sasgd_getMinibatch", "sasgd_pullWeights", "sasgd_calcGradient",
@@ -31,7 +33,7 @@ EXPORTS = [
     "sasgd_copyWeights", "sasgd_copyGradient", "sasgd_copyMomentum", "sasgd_gradientPtr",
     "sasgd_setProfiling", "sasgd_phaseTime", "sasgd_last_error", "sasgd_version",
     "sasgd_evaluate", "sasgd_setBaseRate", "sasgd_setPixelMean", "sasgd_factoredParams",
-    "sasgd_applyUpdateNoAlloc", "sasgd_flush",
+    "sasgd_applyUpdateNoAlloc", "sasgd_flush", "sasgd_gradientNorm", "sasgd_momentElements", "sasgd_applyAdamW",
 ]
 
 
@@ -55,6 +57,20 @@ class SasgdConfig(ctypes.Structure):
         ("in_channels", ctypes.c_int32), ("in_height", ctypes.c_int32), ("in_width", ctypes.c_int32),
         ("alloc", ALLOC_FN), ("release", RELEASE_FN), ("alloc_user", ctypes.c_void_p),
     ]
+
+
+class SasgdAdamw(ctypes.Structure):
+    _fields_ = [("lr_mode", ctypes.c_int32), ("moments", ctypes.c_int32), ("grad_type", ctypes.c_int32), ("seed", ctypes.c_uint32),
+                ("alpha0", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("epsilon", ctypes.c_double),
+                ("weight_decay", ctypes.c_double)]
+
+
+class SasgdTensor(ctypes.Structure):
+    _fields_ = [("numel", ctypes.c_int64), ("theta_in", ctypes.c_void_p), ("theta_out", ctypes.c_void_p), ("shadow_out", ctypes.c_void_p)]
+
+
+class SasgdMoments(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
 class SasgdError(RuntimeError):
@@ -103,6 +119,10 @@ def load():
         lib.sasgd_setPixelMean.argtypes = [vp, vp]
         lib.sasgd_applyUpdateNoAlloc.argtypes = [vp, vp, vp, vp, i64, i32, P(vp), P(i32), i32, ctypes.c_float, ctypes.c_float,
                                                  ctypes.c_float, vp, ctypes.c_char_p, ctypes.c_size_t]
+        lib.sasgd_gradientNorm.argtypes = [P(vp), P(i64), i32, i32, ctypes.c_float, vp, vp, vp, ctypes.c_char_p, ctypes.c_size_t]
+        lib.sasgd_momentElements.argtypes = [P(i64), i32, P(i64)]
+        lib.sasgd_applyAdamW.argtypes = [P(SasgdAdamw), P(SasgdTensor), i32, P(vp), i32, P(i32), P(SasgdMoments), i64, vp, vp, vp, ctypes.c_char_p,
+                                         ctypes.c_size_t]
         lib.sasgd_last_error.argtypes = [vp]
         lib.sasgd_last_error.restype = ctypes.c_char_p
         lib.sasgd_version.restype = ctypes.c_char_p
@@ -302,6 +322,118 @@ def applyUpdateNoAlloc(theta_in_dev, theta_out_dev, v_dev, grads_dev, staleness,
         stream = current_stream()
     return _fast.apply_update_no_alloc(theta_in_dev, theta_out_dev, v_dev, shadow_out_dev, num_params, grads_dev, staleness,
                                        LR_MODES[lr_mode] if isinstance(lr_mode, str) else lr_mode, alpha0, momentum, weight_decay, stream)
+
+
+def _type(dtype):
+    """SASGD_FP32 or SASGD_BF16 of a torch type."""
+    name = str(dtype)
+    if name == "torch.float32":
+        return FP32
+    if name == "torch.bfloat16":
+        return BF16
+    raise TypeError("float32 or bfloat16 tensors are needed, not " + name)
+
+
+def _device():
+    import torch
+    return torch.cuda.current_device()
+
+
+def _want(name, t, types, numel=None):
+    """A contiguous tensor of one of the types (their names) on the current device, of at least `numel` elements where that is given."""
+    if t.get_device() != _device():
+        raise ValueError(name + " is not on the current device")
+    if str(t.dtype)[6:] not in types:
+        raise TypeError("%s must be %s, not %s" % (name, " or ".join(types), t.dtype))
+    if not t.is_contiguous():
+        raise ValueError(name + " must be contiguous")
+    if numel is not None and t.numel() < numel:
+        raise ValueError("%s has %d elements, %d are needed" % (name, t.numel(), numel))
+
+
+def _want_bytes(call, t, size):
+    if t is None or t.numel() * t.element_size() < size or not t.is_contiguous() or t.get_device() != _device():
+        raise ValueError("%s needs a workspace of %d bytes on the current device" % (call, size))
+
+
+def gradientNorm(grads, out, max_norm=0.0, workspace=None, stream=None):
+    """sasgd_gradientNorm: out[0] = the norm over all tensors of the list, out[1] = the factor that bounds it by max_norm (see
+    include/sasgd.h).  grads: contiguous tensors of one type, float32 or bfloat16; out: float32 of two elements; workspace:
+    NORM_WORKSPACE bytes of device memory."""
+    load()
+    dtype = grads[0].dtype if len(grads) else None
+    _want("out", out, ("float32",), 2)
+    _want_bytes("gradientNorm", workspace, NORM_WORKSPACE)
+    _fast.gradient_norm(grads, dtype, FP32 if dtype is None else _type(dtype), max_norm, out, workspace, _device(),
+                        current_stream() if stream is None else stream)
+
+
+def momentElements(weights):
+    """How many elements each moment of these tensors has (sasgd_momentElements)."""
+    numel = (ctypes.c_int64 * max(1, len(weights)))(*[t.numel() for t in weights])
+    out = ctypes.c_int64()
+    rc = load().sasgd_momentElements(numel, len(weights), ctypes.byref(out))
+    if rc != OK:
+        raise SasgdError(rc, "momentElements: tensor lengths out of range")
+    return out.value
+
+
+class AdamW:
+    """sasgd_applyAdamW for a list of weights (see include/sasgd.h): holds the rule and the addresses of weights and moments, which stay the
+    caller's and have to stay alive.
+
+    weights: contiguous float32 tensors; outs: where the new weights go (the weights themselves if not given); copies: optional
+    bfloat16 tensors that receive them too (None for a tensor without).  m, v: of momentElements(weights) elements, float32, or
+    float8_e4m3fn with m_scale and v_scale, float32 of a 256th of that; all zeros at the start."""
+
+    def __init__(self, weights, m, v, m_scale=None, v_scale=None, copies=None, outs=None, alpha0=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
+                 weight_decay=0.0, lr_mode="per_gradient", seed=0):
+        load()
+        weights = list(weights)
+        n = len(weights)
+        outs = weights if outs is None else list(outs)
+        copies = [None] * n if copies is None else list(copies)
+        if len(outs) != n or len(copies) != n:
+            raise ValueError("outs and copies need an entry per tensor")
+        elements = momentElements(weights)
+        self._tensors = (SasgdTensor * max(1, n))()
+        for e, w, o, s in zip(self._tensors, weights, outs, copies):
+            _want("weights", w, ("float32",))
+            _want("outs", o, ("float32",), w.numel())
+            if s is not None:
+                _want("copies", s, ("bfloat16",), w.numel())
+            e.numel, e.theta_in, e.theta_out, e.shadow_out = w.numel(), _addr(w), _addr(o), _addr(s)
+        _want("m", m, ("float32", "float8_e4m3fn"), elements)
+        _want("v", v, (str(m.dtype)[6:],), elements)
+        small = m.element_size() == 1
+        if small:
+            if m_scale is None or v_scale is None:
+                raise ValueError("8-bit moments need their scales")
+            _want("m_scale", m_scale, ("float32",), elements // 256)
+            _want("v_scale", v_scale, ("float32",), elements // 256)
+        self._moments = SasgdMoments(_addr(m), _addr(v), _addr(m_scale) if small else None, _addr(v_scale) if small else None)
+        self._rule = SasgdAdamw(LR_MODES[lr_mode] if isinstance(lr_mode, str) else lr_mode, MOMENTS_E4M3 if small else MOMENTS_FP32, FP32,
+                                seed & 0xFFFFFFFF, alpha0, beta1, beta2, eps, weight_decay)
+        self._keep = (weights, outs, copies, m, v, m_scale, v_scale)
+        self._count = n
+        self._at = (ctypes.addressof(self._rule), ctypes.addressof(self._tensors), ctypes.addressof(self._moments))
+
+    def setBaseRate(self, alpha0):
+        self._rule.alpha0 = alpha0
+
+    def apply(self, grads, step, staleness=None, scale=None, step_dev=None, stream=None):
+        """One step.  grads: c lists of a gradient per tensor, contiguous and of one type, float32 or bfloat16; staleness: one per list
+        (0 if not given); step: 1 in the first step (step_dev: a device int64 tensor that holds it instead); scale: device float, the
+        factor of gradientNorm (its out[1:])."""
+        dtype = grads[0][0].dtype if len(grads) and len(grads[0]) else None
+        if dtype is not None:
+            self._rule.grad_type = _type(dtype)
+        if scale is not None:
+            _want("scale", scale, ("float32",), 1)
+        if step_dev is not None:
+            _want("step_dev", step_dev, ("int64",), 1)
+        _fast.apply_adamw(self._at[0], self._at[1], self._count, self._at[2], grads, dtype, [0] * len(grads) if staleness is None else staleness,
+                          step, step_dev, scale, _device(), current_stream() if stream is None else stream)
 
 
 def current_stream():

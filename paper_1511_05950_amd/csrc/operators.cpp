@@ -1,0 +1,200 @@
+// C entry points of the context-free operators: argument checks and the tables their kernels read.
+#include <math.h>
+#include <stdarg.h>
+#include <stdio.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "../../include/sasgd.h"
+#include "operators.hpp"
+
+using namespace sasgd;
+
+namespace {
+
+int refuse(char* err, size_t err_len, int code, const char* fmt, ...) {
+  if (err && err_len > 0) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(err, err_len, fmt, ap);
+    va_end(ap);
+  }
+  return code;
+}
+#define REFUSE(...) return refuse(err, err_len, SASGD_EINVAL, __VA_ARGS__)
+#define TRY_HIP(x, name)                                                                                     \
+  do {                                                                                                       \
+    const hipError_t e__ = (x);                                                                              \
+    if (e__ != hipSuccess) return refuse(err, err_len, SASGD_EHIP, name ": %s", hipGetErrorString(e__));     \
+  } while (0)
+
+inline int64_t blocks_of(int64_t numel) { return (numel + kMomentBlock - 1) / kMomentBlock; }
+constexpr int64_t kMostElements = (int64_t)1 << 38;     // of a tensor and of a call: a block's number fits 31 bits
+
+}  // namespace
+
+extern "C" {
+
+int sasgd_momentElements(const int64_t* numel, int32_t count, int64_t* out_elements) {
+  if (!out_elements || count < 0 || (count > 0 && !numel)) return SASGD_EINVAL;
+  int64_t blocks = 0;
+  for (int32_t k = 0; k < count; k++) {
+    if (numel[k] < 0 || numel[k] > kMostElements) return SASGD_EINVAL;
+    blocks += blocks_of(numel[k]);
+  }
+  *out_elements = blocks * kMomentBlock;
+  return SASGD_OK;
+}
+
+int sasgd_gradientNorm(const void* const* grads_dev, const int64_t* numel, int32_t count, int32_t type, float max_norm,
+                       float* out_dev, void* workspace_dev, void* stream, char* err, size_t err_len) {
+  if (count < 0 || (count > 0 && (!grads_dev || !numel))) REFUSE("gradientNorm: null array or negative count");
+  if (type != SASGD_FP32 && type != SASGD_BF16) REFUSE("gradientNorm: unknown type");
+  if (!(max_norm >= 0.f)) REFUSE("gradientNorm: max_norm must not be negative");
+  if (!out_dev || ((uintptr_t)out_dev & 3)) REFUSE("gradientNorm: out_dev must be a 4-byte aligned device pointer");
+  if (!workspace_dev || ((uintptr_t)workspace_dev & 7)) REFUSE("gradientNorm: workspace_dev must be an 8-byte aligned device pointer");
+  const bool bf = type == SASGD_BF16;
+  int64_t blocks = 0;
+  for (int32_t k = 0; k < count; k++) {
+    if (numel[k] < 0 || numel[k] > kMostElements) REFUSE("gradientNorm: length of tensor %d out of range", (int)k);
+    if (numel[k] > 0 && (!grads_dev[k] || ((uintptr_t)grads_dev[k] & (bf ? 1 : 3)))) REFUSE("gradientNorm: tensor %d is null or not aligned to its elements", (int)k);
+    blocks += blocks_of(numel[k]);
+  }
+  if (blocks * kMomentBlock > kMostElements) REFUSE("gradientNorm: more than 2^38 elements");
+  static_assert(kNormPartials * sizeof(double) <= SASGD_NORM_WORKSPACE, "partial sums do not fit the workspace");
+  NormLaunch a;
+  memset(&a, 0, sizeof(a));
+  a.partial = (double*)workspace_dev;
+  a.out = out_dev;
+  a.max_norm = max_norm;
+  a.grid = norm_grid(blocks);
+  TensorTable& tab = a.tab;
+  tab.stride = 2;
+  int32_t k = 0;
+  do {
+    tab.n = 0;
+    for (; k < count && tab.n < kTableTensors; k++) {
+      if (numel[k] == 0) continue;
+      uint64_t* w = tab.word + tab.n * 2;
+      const bool aligned = ((uintptr_t)grads_dev[k] & (bf ? 7 : 15)) == 0;
+      w[0] = (uint64_t)numel[k] | (aligned ? kAligned : 0);
+      w[1] = (uint64_t)(uintptr_t)grads_dev[k];
+      tab.first[tab.n + 1] = tab.first[tab.n] + (uint32_t)blocks_of(numel[k]);
+      tab.n++;
+    }
+    TRY_HIP(launch_norm_partials(a, bf, (hipStream_t)stream), "gradientNorm");
+    a.add = 1;
+  } while (k < count);
+  TRY_HIP(launch_norm_finish(a, (hipStream_t)stream), "gradientNorm");
+  return SASGD_OK;
+}
+
+int sasgd_applyAdamW(const sasgd_adamw* rule, const sasgd_tensor* tensors, int32_t count, const void* const* grads_dev, int32_t c,
+                     const int32_t* staleness, const sasgd_moments* moments, int64_t step, const int64_t* step_dev,
+                     const float* factor_dev, void* stream, char* err, size_t err_len) {
+  if (!rule || !moments || !staleness || count < 0 || (count > 0 && (!tensors || !grads_dev))) REFUSE("applyAdamW: null argument or negative count");
+  if (rule->lr_mode < SASGD_LR_PER_GRADIENT || rule->lr_mode > SASGD_LR_CONSTANT) REFUSE("applyAdamW: unknown lr_mode");
+  if (rule->moments != SASGD_MOMENTS_FP32 && rule->moments != SASGD_MOMENTS_E4M3) REFUSE("applyAdamW: unknown type of moments");
+  if (rule->grad_type != SASGD_FP32 && rule->grad_type != SASGD_BF16) REFUSE("applyAdamW: unknown type of gradients");
+  if (!(rule->alpha0 >= 0 && rule->alpha0 < INFINITY && rule->weight_decay >= 0 && rule->weight_decay < INFINITY))
+    REFUSE("applyAdamW: alpha0 and weight_decay must be finite and not negative");
+  if (!(rule->beta1 >= 0 && rule->beta1 < 1 && rule->beta2 >= 0 && rule->beta2 < 1)) REFUSE("applyAdamW: beta1 and beta2 must lie in [0, 1)");
+  if (!(rule->epsilon >= 1e-30 && rule->epsilon < 1e30)) REFUSE("applyAdamW: epsilon must lie in [1e-30, 1e30)");
+  if (c < 1 || c > SASGD_NOALLOC_MAX_GRADIENTS) REFUSE("applyAdamW: c must lie in 1..64");
+  if (step < 1 && !step_dev) REFUSE("applyAdamW: steps count from 1");
+  if (((uintptr_t)step_dev & 7) || ((uintptr_t)factor_dev & 3)) REFUSE("applyAdamW: step_dev and factor_dev must be aligned to their elements");
+  const bool bf = rule->grad_type == SASGD_BF16, e4m3 = rule->moments == SASGD_MOMENTS_E4M3;
+  double sum_tau = 0, sum_a = 0, a_of[SASGD_NOALLOC_MAX_GRADIENTS];
+  for (int l = 0; l < c; l++) {
+    if (staleness[l] < 0) REFUSE("applyAdamW: negative staleness");
+    sum_tau += staleness[l];
+  }
+  for (int l = 0; l < c; l++) {
+    a_of[l] = rule->lr_mode == SASGD_LR_PER_GRADIENT ? 1.0 / std::max(staleness[l], 1)
+              : rule->lr_mode == SASGD_LR_MEAN_STALENESS ? 1.0 / std::max(sum_tau / c, 1.0) : 1.0;
+    sum_a += a_of[l];
+  }
+  bool has_out = false, has_shadow = false;
+  int64_t blocks = 0;
+  for (int32_t k = 0; k < count; k++) {
+    const sasgd_tensor& t = tensors[k];
+    if (t.numel < 0 || t.numel > kMostElements) REFUSE("applyAdamW: length of tensor %d out of range", (int)k);
+    if (t.numel == 0) continue;
+    if (!t.theta_in || !t.theta_out || (((uintptr_t)t.theta_in | (uintptr_t)t.theta_out) & 3) || ((uintptr_t)t.shadow_out & 1))
+      REFUSE("applyAdamW: weights of tensor %d are null or not aligned to their elements", (int)k);
+    for (int l = 0; l < c; l++) {
+      const void* g = grads_dev[(size_t)k * c + l];
+      if (!g || ((uintptr_t)g & (bf ? 1 : 3))) REFUSE("applyAdamW: gradient %d of tensor %d is null or not aligned to its elements", l, (int)k);
+    }
+    has_out = has_out || t.theta_out != t.theta_in;
+    has_shadow = has_shadow || t.shadow_out;
+    blocks += blocks_of(t.numel);
+  }
+  if (blocks * kMomentBlock > kMostElements) REFUSE("applyAdamW: more than 2^38 elements");
+  if (blocks == 0) return SASGD_OK;
+  if (!moments->m || !moments->v || (((uintptr_t)moments->m | (uintptr_t)moments->v) & 15)) REFUSE("applyAdamW: moments must be 16-byte aligned device pointers");
+  if (e4m3 && (!moments->m_scale || !moments->v_scale || (((uintptr_t)moments->m_scale | (uintptr_t)moments->v_scale) & 3)))
+    REFUSE("applyAdamW: e4m3 moments need 4-byte aligned scales");
+  AdamwLaunch a;
+  memset(&a, 0, sizeof(a));
+  a.c = c;
+  a.has_out = has_out;
+  a.has_shadow = has_shadow;
+  a.grads_at = 2 + a.has_out + a.has_shadow;
+  a.words_at = (c + 1) / 2;
+  a.seed = rule->seed;
+  a.m = moments->m;
+  a.v = moments->v;
+  a.m_scale = moments->m_scale;
+  a.v_scale = moments->v_scale;
+  a.factor = factor_dev;
+  a.step_dev = step_dev;
+  a.step = step;
+  a.rate = rule->alpha0 * (sum_a / c);
+  a.log_beta1 = log(rule->beta1);          // -inf for 0: 1 - beta^t is 1
+  a.log_beta2 = log(rule->beta2);
+  if (!step_dev) {
+    a.pace = (float)(a.rate / -expm1((double)step * a.log_beta1));
+    a.vcorr = (float)(1.0 / -expm1((double)step * a.log_beta2));
+  }
+  a.beta1 = (float)rule->beta1;
+  a.rest1 = (float)(1.0 - rule->beta1);
+  a.beta2 = (float)rule->beta2;
+  a.rest2 = (float)(1.0 - rule->beta2);
+  a.epsilon = (float)rule->epsilon;
+  a.keep = (float)(1.0 - a.rate * rule->weight_decay);
+  TensorTable& tab = a.tab;
+  for (int l = 0; l < c; l++) {
+    const float share = (float)(a_of[l] / sum_a);
+    memcpy((char*)tab.word + 4 * l, &share, 4);
+  }
+  tab.stride = a.grads_at + c;
+  const int most = std::min(kTableTensors, (kTableWords - a.words_at) / tab.stride);
+  for (int32_t k = 0; k < count;) {
+    tab.n = 0;
+    for (; k < count && tab.n < most; k++) {
+      const sasgd_tensor& t = tensors[k];
+      if (t.numel == 0) continue;
+      uint64_t* w = tab.word + a.words_at + tab.n * tab.stride;
+      uintptr_t low = (uintptr_t)t.theta_in | (uintptr_t)t.theta_out | ((uintptr_t)t.shadow_out << 1);
+      w[1] = (uint64_t)(uintptr_t)t.theta_in;
+      if (has_out) w[2] = (uint64_t)(uintptr_t)t.theta_out;
+      if (has_shadow) w[2 + a.has_out] = (uint64_t)(uintptr_t)t.shadow_out;
+      for (int l = 0; l < c; l++) {
+        const uintptr_t g = (uintptr_t)grads_dev[(size_t)k * c + l];
+        low |= bf ? g << 1 : g;
+        w[a.grads_at + l] = (uint64_t)g;
+      }
+      w[0] = (uint64_t)t.numel | ((low & 15) == 0 ? kAligned : 0);
+      tab.first[tab.n + 1] = tab.first[tab.n] + (uint32_t)blocks_of(t.numel);
+      tab.n++;
+    }
+    if (tab.n == 0) break;
+    TRY_HIP(launch_adamw(a, bf, e4m3, (hipStream_t)stream), "applyAdamW");
+    a.block0 += tab.first[tab.n];
+  }
+  return SASGD_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,55 @@
+// Launches of the context-free operators (operators.cpp checks their arguments).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sasgd {
+
+// ---------------------------------------------------------------- many tensors (adamw.hip)
+constexpr int kMomentBlock = 256;        // consecutive elements of a tensor that share a scale
+constexpr int kTableTensors = 100;       // of one launch
+constexpr int kTableWords = 416;
+// The tensors of one launch, passed by value (kernel arguments hold 4 KiB).  first[k]: block at which tensor k begins,
+// first[n] the number of blocks; empty tensors are left out.  word: per tensor `stride` words, see TensorWords.
+struct TensorTable {
+  uint64_t word[kTableWords];
+  uint32_t first[kTableTensors + 1];
+  int32_t n, stride;
+};
+// A tensor's words: its length, its first pointer, then what the launch has (theta_out, shadow, further gradients).
+// The length's top bit: every pointer of the tensor is aligned for vector moves.
+constexpr uint64_t kAligned = (uint64_t)1 << 63;
+
+struct AdamwLaunch {
+  TensorTable tab;           // words of a tensor: numel, theta_in, [theta_out], [shadow], g_0 .. g_{c-1}; the c shares (float) come first
+  int32_t c, has_out, has_shadow, grads_at;   // grads_at: a tensor's word with g_0;  tensors' words begin behind the shares
+  int32_t words_at;
+  uint32_t seed;
+  int64_t block0;            // moments' block of the launch's first block
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  const float* factor;
+  const int64_t* step_dev;
+  int64_t step;
+  double rate, log_beta1, log_beta2;
+  float pace, vcorr;         // rate / (1 - beta1^step), 1 / (1 - beta2^step); computed from step_dev where there is one
+  float beta1, rest1, beta2, rest2, epsilon, keep;   // rest = 1 - beta, keep = 1 - rate weight_decay
+};
+hipError_t launch_adamw(const AdamwLaunch& a, bool grad_bf16, bool e4m3, hipStream_t stream);
+
+constexpr int kNormPartials = 2048;
+struct NormLaunch {
+  TensorTable tab;           // words of a tensor: numel, gradient
+  double* partial;           // [grid]
+  float* out;                // norm, factor
+  float max_norm;
+  int32_t add;               // partial[] holds the sums of the launches before
+  int32_t grid;
+};
+int norm_grid(int64_t blocks);
+hipError_t launch_norm_partials(const NormLaunch& a, bool bf16, hipStream_t stream);
+hipError_t launch_norm_finish(const NormLaunch& a, hipStream_t stream);
+
+}  // namespace sasgd

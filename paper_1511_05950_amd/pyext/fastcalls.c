@@ -13,6 +13,10 @@ static PyObject* error_class;     /* binding.SasgdError(code, message) */
 static PyObject* s_data_ptr;      /* "data_ptr" */
 static PyObject* s_ctypes;        /* "ctypes" */
 static PyObject* s_data;          /* "data" */
+static PyObject* s_dtype;         /* "dtype" */
+static PyObject* s_numel;         /* "numel" */
+static PyObject* s_is_contiguous; /* "is_contiguous" */
+static PyObject* s_get_device;    /* "get_device" */
 
 static PyObject* raise_code(int code, const char* msg) {
   PyObject* exc = PyObject_CallFunction(error_class, "is", code, msg);
@@ -253,6 +257,160 @@ static PyObject* apply_update_no_alloc(PyObject* self, PyObject* const* a, Py_ss
   return PyLong_FromLong(rc);
 }
 
+/* One tensor of a list: its address, checked to be a contiguous tensor of `dtype` on device number `device`; its length into *numel, or
+ * checked against it where that is not negative. */
+static int list_tensor(PyObject* o, PyObject* dtype, long device, int64_t* numel, void** out) {
+  PyObject* v;
+  long long n;
+  int same;
+  v = PyObject_CallMethodNoArgs(o, s_get_device);
+  if (!v) return -1;
+  n = PyLong_AsLongLong(v);
+  Py_DECREF(v);
+  if (n == -1 && PyErr_Occurred()) return -1;
+  if (n != device) {
+    PyErr_SetString(PyExc_ValueError, "a tensor is not on the current device");
+    return -1;
+  }
+  v = PyObject_GetAttr(o, s_dtype);
+  if (!v) return -1;
+  same = v == dtype;
+  Py_DECREF(v);
+  if (!same) {
+    PyErr_SetString(PyExc_TypeError, "tensors of another type than the first one's");
+    return -1;
+  }
+  v = PyObject_CallMethodNoArgs(o, s_is_contiguous);
+  if (!v) return -1;
+  same = v == Py_True;
+  Py_DECREF(v);
+  if (!same) {
+    PyErr_SetString(PyExc_ValueError, "a tensor is not contiguous");
+    return -1;
+  }
+  v = PyObject_CallMethodNoArgs(o, s_numel);
+  if (!v) return -1;
+  n = PyLong_AsLongLong(v);
+  Py_DECREF(v);
+  if (n == -1 && PyErr_Occurred()) return -1;
+  if (*numel >= 0 && n != *numel) {
+    PyErr_SetString(PyExc_ValueError, "a gradient's length is not its tensor's");
+    return -1;
+  }
+  *numel = n;
+  return address(o, out);
+}
+
+/* gradient_norm(grads, dtype, type, max_norm, out, workspace, device, stream) */
+static PyObject* gradient_norm(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  int32_t type, device;
+  double max_norm;
+  void *out, *work, *stream;
+  Py_ssize_t n, k;
+  PyObject* seq;
+  const void** grads;
+  int64_t* numel;
+  char err[256] = "";
+  int rc, bad = 0;
+  NARGS(8);
+  if (integer32(a[2], &type) || address(a[4], &out) || address(a[5], &work) || integer32(a[6], &device) || address(a[7], &stream)) return NULL;
+  max_norm = PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred()) return NULL;
+  seq = PySequence_Fast(a[0], "grads must be a sequence");
+  if (!seq) return NULL;
+  n = PySequence_Fast_GET_SIZE(seq);
+  if (n > INT32_MAX) {
+    Py_DECREF(seq);
+    return raise_code(SASGD_EINVAL, "gradientNorm: too many tensors");
+  }
+  grads = (const void**)PyMem_Malloc(sizeof(void*) * (size_t)(n ? n : 1));
+  numel = (int64_t*)PyMem_Malloc(sizeof(int64_t) * (size_t)(n ? n : 1));
+  bad = !grads || !numel;
+  if (bad) PyErr_NoMemory();
+  for (k = 0; !bad && k < n; k++) {
+    numel[k] = -1;
+    bad = list_tensor(PySequence_Fast_GET_ITEM(seq, k), a[1], device, &numel[k], (void**)&grads[k]);
+  }
+  Py_DECREF(seq);
+  rc = 0;
+  if (!bad) {
+    Py_BEGIN_ALLOW_THREADS
+    rc = sasgd_gradientNorm(grads, numel, (int32_t)n, type, (float)max_norm, (float*)out, work, stream, err, sizeof(err));
+    Py_END_ALLOW_THREADS
+  }
+  PyMem_Free(grads);
+  PyMem_Free(numel);
+  if (bad) return NULL;
+  if (rc) return raise_code(rc, err);
+  Py_RETURN_NONE;
+}
+
+/* apply_adamw(rule, tensors, count, moments, grads, dtype, staleness, step, step_dev, factor, device, stream): rule, tensors and moments are addresses
+ * of the C structures, grads a sequence of c sequences of `count` tensors. */
+static PyObject* apply_adamw(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  void *rule, *tensors, *moments, *step_dev, *factor, *stream;
+  int32_t count, device, stale[SASGD_NOALLOC_MAX_GRADIENTS];
+  long long step;
+  Py_ssize_t c, l, k;
+  PyObject *lists, *st;
+  const void** grads = NULL;
+  char err[256] = "";
+  int rc = 0, bad = 0;
+  NARGS(12);
+  if (address(a[0], &rule) || address(a[1], &tensors) || integer32(a[2], &count) || address(a[3], &moments) || integer(a[7], &step) ||
+      address(a[8], &step_dev) || address(a[9], &factor) || integer32(a[10], &device) || address(a[11], &stream))
+    return NULL;
+  lists = PySequence_Fast(a[4], "grads must be a sequence of sequences");
+  if (!lists) return NULL;
+  st = PySequence_Fast(a[6], "staleness must be a sequence");
+  if (!st) {
+    Py_DECREF(lists);
+    return NULL;
+  }
+  c = PySequence_Fast_GET_SIZE(lists);
+  if (c < 1 || c > SASGD_NOALLOC_MAX_GRADIENTS || PySequence_Fast_GET_SIZE(st) != c) {
+    Py_DECREF(lists);
+    Py_DECREF(st);
+    return raise_code(SASGD_EINVAL, "applyAdamW: 1..64 gradients and as many staleness values are needed");
+  }
+  for (l = 0; !bad && l < c; l++) bad = as_integer32(PySequence_Fast_GET_ITEM(st, l), &stale[l]);
+  Py_DECREF(st);
+  if (!bad) {
+    grads = (const void**)PyMem_Malloc(sizeof(void*) * (size_t)(count > 0 ? count : 1) * (size_t)c);
+    if (!grads) {
+      PyErr_NoMemory();
+      bad = 1;
+    }
+  }
+  for (l = 0; !bad && l < c; l++) {
+    PyObject* one = PySequence_Fast(PySequence_Fast_GET_ITEM(lists, l), "grads must be a sequence of sequences");
+    if (!one) {
+      bad = 1;
+      break;
+    }
+    if (PySequence_Fast_GET_SIZE(one) != count) {
+      PyErr_SetString(PyExc_ValueError, "a gradient has another number of tensors than the weights");
+      bad = 1;
+    }
+    for (k = 0; !bad && k < count; k++) {
+      int64_t numel = ((const sasgd_tensor*)tensors)[k].numel;
+      bad = list_tensor(PySequence_Fast_GET_ITEM(one, k), a[5], device, &numel, (void**)&grads[k * c + l]);
+    }
+    Py_DECREF(one);
+  }
+  Py_DECREF(lists);
+  if (!bad) {
+    Py_BEGIN_ALLOW_THREADS
+    rc = sasgd_applyAdamW((const sasgd_adamw*)rule, (const sasgd_tensor*)tensors, count, grads, (int32_t)c, stale, (const sasgd_moments*)moments, step,
+                          (const int64_t*)step_dev, (const float*)factor, stream, err, sizeof(err));
+    Py_END_ALLOW_THREADS
+  }
+  PyMem_Free(grads);
+  if (bad) return NULL;
+  if (rc) return raise_code(rc, err);
+  Py_RETURN_NONE;
+}
+
 static PyObject* set_error_class(PyObject* self, PyObject* cls) {
   Py_INCREF(cls);
   Py_XDECREF(error_class);
@@ -267,6 +425,8 @@ static PyMethodDef methods[] = {FAST(get_minibatch),
                                 FAST(push_gradient_external),
                                 FAST(calc_gradient),
                                 FAST(apply_update_no_alloc),
+                                FAST(gradient_norm),
+                                FAST(apply_adamw),
                                 {"sum_gradients", sum_gradients, METH_O, NULL},
                                 {"apply_update", apply_update, METH_O, NULL},
                                 {"timestamp", timestamp, METH_O, NULL},
@@ -279,7 +439,11 @@ PyMODINIT_FUNC PyInit__fastcalls(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_ctypes = PyUnicode_InternFromString("ctypes");
   s_data = PyUnicode_InternFromString("data");
-  if (!s_data_ptr || !s_ctypes || !s_data) return NULL;
+  s_dtype = PyUnicode_InternFromString("dtype");
+  s_numel = PyUnicode_InternFromString("numel");
+  s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+  s_get_device = PyUnicode_InternFromString("get_device");
+  if (!s_data_ptr || !s_ctypes || !s_data || !s_dtype || !s_numel || !s_is_contiguous || !s_get_device) return NULL;
   Py_INCREF(PyExc_RuntimeError);
   error_class = PyExc_RuntimeError;
   return PyModule_Create(&module);
