@@ -265,6 +265,45 @@ int sasgd_applyAdamW(const sasgd_adamw* rule, const sasgd_tensor* tensors, int32
                      const int32_t* staleness, const sasgd_moments* moments, int64_t step, const int64_t* step_dev,
                      const float* factor_dev, void* stream, char* err, size_t err_len);
 
+/* ---- group normalisation ------------------------------------------------------------------ */
+
+/* Group normalisation of activations with the channels last, and the activation behind it, context-free like the calls above (same rules
+ * for streams, errors and graphs; nothing is allocated).  For every image and every group of channels / groups consecutive channels, over
+ * the m = positions channels / groups values:
+ *     mean = sum x / m;   r = 1 / sqrt(sum (x - mean)^2 / m + eps);   z = (x - mean) r scale + shift;   y = act(z)
+ * Value c of position p of image n lies at x + n x_image + p x_pixel + c (elements; dx like x), and likewise for y (dy like y); a stride
+ * of 0 stands for a dense tensor.  Pointers need the alignment of their elements; where channels, strides and pointers are whole 16 bytes,
+ * 16 are moved at a time. */
+enum { SASGD_ACT_NONE = 0, SASGD_ACT_RELU = 1, SASGD_ACT_SILU = 2 };   /* silu(z) = z / (1 + exp(-z)); relu'(0) = 0 */
+typedef struct {
+  int64_t images;           /* >= 0                                                                       */
+  int64_t positions;        /* height x width, 1 .. 2^26                                                  */
+  int32_t channels, groups; /* groups divides channels; at most 4096 channels, or 1024 where they are not moved 16 bytes at a time */
+  int32_t type;             /* SASGD_FP32 or SASGD_BF16: of x, y, dy, dx; sums and statistics are fp32    */
+  int32_t param_type;       /* of scale and shift (their gradients are fp32)                              */
+  int32_t activation;       /* SASGD_ACT_*                                                                */
+  float eps;                /* > 0                                                                        */
+  int64_t x_image, x_pixel, y_image, y_pixel;
+} sasgd_norm_shape;
+
+/* Bytes of workspace that groupNorm (gradient 0) or groupNormGradient (1) needs for this shape, whatever its strides and alignment; may be 0. */
+int sasgd_groupNormWorkspace(const sasgd_norm_shape* shape, int32_t gradient, size_t* out_bytes);
+
+/* groupNorm.  scale, shift: device [channels], or NULL for ones and zeros.  stats_dev: optional device float32 [images][groups][2], receives
+ * mean and r, which the backward pass needs.  y_dev may be x_dev (with x's strides).  workspace_dev: 16-byte aligned, any contents.
+ * Errors: EINVAL (argument), EHIP. */
+int sasgd_groupNorm(const sasgd_norm_shape* shape, const void* x_dev, const void* scale_dev, const void* shift_dev, void* y_dev, float* stats_dev,
+                    void* workspace_dev, size_t workspace_bytes, void* stream, char* err, size_t err_len);
+
+/* groupNormGradient: with dz = dy act'(z) and xhat = (x - mean) r
+ *     dshift = sum dz;   dscale = sum dz xhat   over images and positions, in a fixed order;
+ *     dx = r (scale dz - (sum scale dz + xhat sum scale dz xhat) / m)   the sums over the group
+ * z is computed again, with the rounding of the forward pass.  dx_dev, dscale_dev, dshift_dev (float32 [channels]): each optional; dx_dev may
+ * be dy_dev.  No images: dscale and dshift become 0.  Errors: EINVAL (argument), EHIP. */
+int sasgd_groupNormGradient(const sasgd_norm_shape* shape, const void* x_dev, const void* scale_dev, const void* shift_dev, const float* stats_dev,
+                            const void* dy_dev, void* dx_dev, float* dscale_dev, float* dshift_dev, void* workspace_dev, size_t workspace_bytes,
+                            void* stream, char* err, size_t err_len);
+
 /* ---- training-loop pieces around the hot path (Sections 4.1 - 4.3) ---------------------- */
 
 /* evaluate: forward pass only over the bound mini-batches of the listed learners, each on its

@@ -23,6 +23,7 @@ LR_MODES = {"per_gradient": 0, "mean_staleness": 1, "constant": 2}
 FLAG_FLAT_FC_GRADIENT = 1
 FLAG_EAGER_UPDATES = 2
 COMPUTE = {"fp32": 0, "bf16": 1}
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
 MOMENTS_FP32, MOMENTS_E4M3 = 0, 1
 NORM_WORKSPACE = 16384
 
@@ -34,6 +35,7 @@ EXPORTS = [
     "sasgd_setProfiling", "sasgd_phaseTime", "sasgd_last_error", "sasgd_version",
     "sasgd_evaluate", "sasgd_setBaseRate", "sasgd_setPixelMean", "sasgd_factoredParams",
     "sasgd_applyUpdateNoAlloc", "sasgd_flush", "sasgd_gradientNorm", "sasgd_momentElements", "sasgd_applyAdamW",
+    "sasgd_groupNorm", "sasgd_groupNormGradient", "sasgd_groupNormWorkspace",
 ]
 
 
@@ -57,6 +59,12 @@ class SasgdConfig(ctypes.Structure):
         ("in_channels", ctypes.c_int32), ("in_height", ctypes.c_int32), ("in_width", ctypes.c_int32),
         ("alloc", ALLOC_FN), ("release", RELEASE_FN), ("alloc_user", ctypes.c_void_p),
     ]
+
+
+class SasgdNormShape(ctypes.Structure):
+    _fields_ = [("images", ctypes.c_int64), ("positions", ctypes.c_int64), ("channels", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("param_type", ctypes.c_int32), ("activation", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("x_image", ctypes.c_int64), ("x_pixel", ctypes.c_int64), ("y_image", ctypes.c_int64), ("y_pixel", ctypes.c_int64)]
 
 
 class SasgdAdamw(ctypes.Structure):
@@ -119,6 +127,10 @@ def load():
         lib.sasgd_setPixelMean.argtypes = [vp, vp]
         lib.sasgd_applyUpdateNoAlloc.argtypes = [vp, vp, vp, vp, i64, i32, P(vp), P(i32), i32, ctypes.c_float, ctypes.c_float,
                                                  ctypes.c_float, vp, ctypes.c_char_p, ctypes.c_size_t]
+        shape = P(SasgdNormShape)
+        lib.sasgd_groupNormWorkspace.argtypes = [shape, i32, P(ctypes.c_size_t)]
+        lib.sasgd_groupNorm.argtypes = [shape, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, ctypes.c_char_p, ctypes.c_size_t]
+        lib.sasgd_groupNormGradient.argtypes = [shape, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, ctypes.c_char_p, ctypes.c_size_t]
         lib.sasgd_gradientNorm.argtypes = [P(vp), P(i64), i32, i32, ctypes.c_float, vp, vp, vp, ctypes.c_char_p, ctypes.c_size_t]
         lib.sasgd_momentElements.argtypes = [P(i64), i32, P(i64)]
         lib.sasgd_applyAdamW.argtypes = [P(SasgdAdamw), P(SasgdTensor), i32, P(vp), i32, P(i32), P(SasgdMoments), i64, vp, vp, vp, ctypes.c_char_p,
@@ -354,6 +366,96 @@ def _want(name, t, types, numel=None):
 def _want_bytes(call, t, size):
     if t is None or t.numel() * t.element_size() < size or not t.is_contiguous() or t.get_device() != _device():
         raise ValueError("%s needs a workspace of %d bytes on the current device" % (call, size))
+
+
+def _pixels(name, t):
+    """(images, positions, channels, image stride, pixel stride) of a tensor [images][height][width][channels] (or without width, or
+    without both): channels side by side, positions evenly apart."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) < 2:
+        raise ValueError(name + " must be [images, ..., channels]")
+    c = shape[-1]
+    positions, pixel = 1, c
+    if c > 1 and stride[-1] != 1:
+        raise ValueError(name + ": channels must be the last dimension, side by side")
+    for n, s in zip(reversed(shape[1:-1]), reversed(stride[1:-1])):
+        if n == 1:
+            continue
+        if positions == 1:
+            pixel = s
+        elif s != pixel * positions:
+            raise ValueError(name + ": positions must be evenly apart")
+        positions *= n
+    return shape[0], positions, c, stride[0] if shape[0] > 1 else pixel * positions, pixel
+
+
+def _norm_shape(x, y, groups, scale, activation, eps):
+    n, p, c, xi, xp = _pixels("x", x)
+    yi, yp = 0, 0
+    if y is not None:
+        if y.shape != x.shape or y.dtype is not x.dtype:
+            raise ValueError("x, y and the gradients must have one shape and one type")
+        _, _, _, yi, yp = _pixels("y", y)
+    return SasgdNormShape(n, p, c, groups, _type(x.dtype), FP32 if scale is None else _type(scale.dtype),
+                          ACTIVATIONS[activation] if isinstance(activation, str) else activation, eps, xi, xp, yi, yp)
+
+
+def _norm_tensors(x, scale, shift, stats, groups, *others):
+    device = _device()
+    for name, t in (("scale", scale), ("shift", shift)):
+        if t is not None:
+            if t.numel() != x.shape[-1] or not t.is_contiguous():
+                raise ValueError(name + " must have one value per channel")
+            if scale is not None and t.dtype is not scale.dtype or scale is None and str(t.dtype) != "torch.float32":
+                raise TypeError("scale and shift must have one type, a shift alone float32")
+    if stats is not None:
+        _want("stats", stats, ("float32",), 2 * x.shape[0] * groups)
+    for t in (x, scale, shift) + others:
+        if t is not None and t.get_device() != device:
+            raise ValueError("a tensor is not on the current device")
+
+
+def groupNormWorkspace(x, groups, gradient=False):
+    """Bytes of workspace that groupNorm (groupNormGradient) needs for x [images, height, width, channels]."""
+    out = ctypes.c_size_t()
+    rc = load().sasgd_groupNormWorkspace(ctypes.byref(_norm_shape(x, None, groups, None, 0, 1e-5)), 1 if gradient else 0, ctypes.byref(out))
+    if rc != OK:
+        raise SasgdError(rc, "groupNormWorkspace: bad shape")
+    return out.value
+
+
+def groupNorm(x, scale, shift, groups, y, stats=None, activation="none", eps=1e-5, workspace=None, stream=None):
+    """sasgd_groupNorm: group normalisation of x [images, height, width, channels] and the activation behind it, into y (see
+    include/sasgd.h).  x, y: float32 or bfloat16, channels side by side, pixels evenly apart (a slice of a wider tensor's channels will do);
+    scale, shift: a value per channel, or None; stats: float32 [images, groups, 2] for the backward pass, or None; workspace:
+    groupNormWorkspace bytes (None where that is 0)."""
+    lib = load()
+    _norm_tensors(x, scale, shift, stats, groups, y, workspace)
+    err = ctypes.create_string_buffer(256)
+    rc = lib.sasgd_groupNorm(ctypes.byref(_norm_shape(x, y, groups, scale if scale is not None else shift, activation, eps)), x.data_ptr(), _addr(scale), _addr(shift), y.data_ptr(),
+                             _addr(stats), _addr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                             current_stream() if stream is None else stream, err, 256)
+    if rc != OK:
+        raise SasgdError(rc, err.value.decode())
+
+
+def groupNormGradient(x, scale, shift, groups, stats, dy, dx=None, dscale=None, dshift=None, activation="none", workspace=None, stream=None):
+    """sasgd_groupNormGradient: dx, dscale and dshift (each optional) of groupNorm's inputs from its output's gradient dy and the
+    statistics it has kept.  dx has the strides of dy."""
+    lib = load()
+    _norm_tensors(x, scale, shift, stats, groups, dy, dx, dscale, dshift, workspace)
+    shape = _norm_shape(x, dy, groups, scale if scale is not None else shift, activation, 1e-5)
+    if dx is not None and (dx.shape != x.shape or dx.dtype is not x.dtype or _pixels("dx", dx) != _pixels("dy", dy)):
+        raise ValueError("dx must have the shape, type and strides of dy")
+    for name, t in (("dscale", dscale), ("dshift", dshift)):
+        if t is not None:
+            _want(name, t, ("float32",), x.shape[-1])
+    err = ctypes.create_string_buffer(256)
+    rc = lib.sasgd_groupNormGradient(ctypes.byref(shape), x.data_ptr(), _addr(scale), _addr(shift), stats.data_ptr(), dy.data_ptr(), _addr(dx), _addr(dscale),
+                                     _addr(dshift), _addr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                     current_stream() if stream is None else stream, err, 256)
+    if rc != OK:
+        raise SasgdError(rc, err.value.decode())
 
 
 def gradientNorm(grads, out, max_norm=0.0, workspace=None, stream=None):

@@ -30,11 +30,119 @@ int refuse(char* err, size_t err_len, int code, const char* fmt, ...) {
   } while (0)
 
 inline int64_t blocks_of(int64_t numel) { return (numel + kMomentBlock - 1) / kMomentBlock; }
-constexpr int64_t kMostElements = (int64_t)1 << 38;     // of a tensor and of a call: a block's number fits 31 bits
+constexpr int64_t kMostElements = (int64_t)1 << 35;     // of a tensor and of a call: its launch stays below 2^32 lanes
+
+// ---------------------------------------------------------------- group normalisation
+constexpr int kWideChannels = 4096, kNarrowChannels = 1024;   // sums by channel of a workgroup lie in LDS
+
+const char* shape_error(const sasgd_norm_shape* s) {
+  if (!s) return "null shape";
+  if (s->images < 0 || s->positions < 1 || s->positions > ((int64_t)1 << 26)) return "images or positions out of range";
+  if (s->channels < 1 || s->channels > kWideChannels || s->groups < 1 || s->channels % s->groups != 0) return "channels must be 1..4096 and a multiple of groups";
+  if ((s->type != SASGD_FP32 && s->type != SASGD_BF16) || (s->param_type != SASGD_FP32 && s->param_type != SASGD_BF16)) return "unknown type";
+  if (s->activation < SASGD_ACT_NONE || s->activation > SASGD_ACT_SILU) return "unknown activation";
+  if (!(s->eps > 0.f && s->eps < INFINITY)) return "eps must be positive and finite";
+  if (s->x_image < 0 || s->x_pixel < 0 || s->y_image < 0 || s->y_pixel < 0) return "negative stride";
+  if ((s->x_pixel && s->x_pixel < s->channels) || (s->y_pixel && s->y_pixel < s->channels)) return "pixels overlap";
+  return nullptr;
+}
+
+GroupNormShape inner_shape(const sasgd_norm_shape& s) { return GroupNormShape{s.images, (int)s.positions, s.channels, s.groups, s.type == SASGD_BF16}; }
+
+size_t align16(size_t n) { return (n + 15) & ~(size_t)15; }
+
+size_t need_bytes(const GroupNormShape& s, const GroupNormPlan& p, bool gradient) {
+  return align16(group_norm_part_bytes(s, p)) + (gradient ? group_norm_sum_bytes(s, p) : 0);
+}
+
+// Checks what both directions have in common and fills the launch's arguments; nullptr if all is well.
+const char* group_norm_args(const sasgd_norm_shape* shape, const void* x, const void* y, const void* dx, const void* scale, const void* shift,
+                            void* work, size_t work_bytes, bool gradient, GroupNormArgs& a) {
+  const char* e = shape_error(shape);
+  if (e) return e;
+  memset(&a, 0, sizeof(a));
+  a.s = inner_shape(*shape);
+  a.learners = 1;
+  a.activation = shape->activation;
+  a.eps = shape->eps;
+  const int size = a.s.bf16 ? 2 : 4;
+  a.x_pixel = shape->x_pixel ? shape->x_pixel : shape->channels;
+  a.y_pixel = shape->y_pixel ? shape->y_pixel : shape->channels;
+  a.x_image = shape->x_image ? shape->x_image : a.x_pixel * shape->positions;
+  a.y_image = shape->y_image ? shape->y_image : a.y_pixel * shape->positions;
+  if (a.x_pixel > ((int64_t)1 << 32) || a.y_pixel > ((int64_t)1 << 32) || a.x_image > ((int64_t)1 << 40) || a.y_image > ((int64_t)1 << 40)) return "stride out of range";
+  if (a.s.images > ((int64_t)1 << 31)) return "too many images for a launch";
+  if (shape->images > 0 && (!x || !y)) return "null tensor";
+  const uintptr_t low = (uintptr_t)x | (uintptr_t)y | (uintptr_t)dx;
+  if (low & (size - 1)) return "tensors must be aligned to their elements";
+  const int psize = shape->param_type == SASGD_BF16 ? 2 : 4;
+  if (((uintptr_t)scale | (uintptr_t)shift) & (psize - 1)) return "scale and shift must be aligned to their elements";
+  const int vec = 16 / size;
+  const bool wide = (low & 15) == 0 && (a.s.channels | a.x_pixel | a.y_pixel | a.x_image | a.y_image) % vec == 0;
+  if (!wide && a.s.channels > kNarrowChannels) return "more than 1024 channels must be whole 16 bytes, in strides and pointers too";
+  a.plan = group_norm_plan(a.s, wide, gradient, 1);
+  if (a.s.images * (int64_t)(a.plan.whole ? a.plan.slabs : a.plan.chunks) * a.plan.threads >= ((int64_t)1 << 32)) return "too many images for a launch";
+  const size_t need = need_bytes(a.s, a.plan, gradient);
+  if (need > 0 && (!work || ((uintptr_t)work & 15) || work_bytes < need)) return "workspace missing, too small or not 16-byte aligned";
+  a.x = (int64_t)(uintptr_t)x;
+  (gradient ? a.dy : a.y) = (int64_t)(uintptr_t)y;
+  a.dx = (int64_t)(uintptr_t)dx;
+  a.parts = (int64_t)(uintptr_t)work;
+  a.sums = a.parts + (int64_t)align16(group_norm_part_bytes(a.s, a.plan));
+  a.scale = (int64_t)(uintptr_t)scale;
+  a.shift = (int64_t)(uintptr_t)shift;
+  a.has_scale = scale != nullptr;
+  a.has_shift = shift != nullptr;
+  a.param_bf16 = shape->param_type == SASGD_BF16;
+  return nullptr;
+}
 
 }  // namespace
 
 extern "C" {
+
+int sasgd_groupNormWorkspace(const sasgd_norm_shape* shape, int32_t gradient, size_t* out_bytes) {
+  if (!out_bytes || shape_error(shape)) return SASGD_EINVAL;
+  const GroupNormShape s = inner_shape(*shape);
+  size_t most = 0;
+  for (int wide = 0; wide < 2; wide++) {
+    if (wide && s.channels % (s.bf16 ? 8 : 4) != 0) continue;
+    if (!wide && s.channels > kNarrowChannels) continue;
+    most = std::max(most, need_bytes(s, group_norm_plan(s, wide != 0, gradient != 0, 1), gradient != 0));
+  }
+  *out_bytes = most;
+  return SASGD_OK;
+}
+
+int sasgd_groupNorm(const sasgd_norm_shape* shape, const void* x_dev, const void* scale_dev, const void* shift_dev, void* y_dev, float* stats_dev,
+                    void* workspace_dev, size_t workspace_bytes, void* stream, char* err, size_t err_len) {
+  GroupNormArgs a;
+  const char* e = group_norm_args(shape, x_dev, y_dev, nullptr, scale_dev, shift_dev, workspace_dev, workspace_bytes, false, a);
+  if (e) REFUSE("groupNorm: %s", e);
+  if ((uintptr_t)stats_dev & 7) REFUSE("groupNorm: stats_dev must be 8-byte aligned");
+  a.stats = (int64_t)(uintptr_t)stats_dev;
+  a.has_stats = stats_dev != nullptr;
+  TRY_HIP(launch_group_norm(a, (hipStream_t)stream), "groupNorm");
+  return SASGD_OK;
+}
+
+int sasgd_groupNormGradient(const sasgd_norm_shape* shape, const void* x_dev, const void* scale_dev, const void* shift_dev, const float* stats_dev,
+                            const void* dy_dev, void* dx_dev, float* dscale_dev, float* dshift_dev, void* workspace_dev, size_t workspace_bytes,
+                            void* stream, char* err, size_t err_len) {
+  GroupNormArgs a;
+  const char* e = group_norm_args(shape, x_dev, dy_dev, dx_dev, scale_dev, shift_dev, workspace_dev, workspace_bytes, true, a);
+  if (e) REFUSE("groupNormGradient: %s", e);
+  if ((shape->images > 0 && !stats_dev) || ((uintptr_t)stats_dev & 7)) REFUSE("groupNormGradient: stats_dev must be an 8-byte aligned device pointer");
+  if (((uintptr_t)dscale_dev | (uintptr_t)dshift_dev) & 3) REFUSE("groupNormGradient: dscale_dev and dshift_dev must be 4-byte aligned");
+  a.stats = (int64_t)(uintptr_t)stats_dev;
+  a.has_dx = dx_dev != nullptr;
+  a.dscale = (int64_t)(uintptr_t)dscale_dev;
+  a.dshift = (int64_t)(uintptr_t)dshift_dev;
+  a.has_dscale = dscale_dev != nullptr;
+  a.has_dshift = dshift_dev != nullptr;
+  TRY_HIP(launch_group_norm_gradient(a, (hipStream_t)stream), "groupNormGradient");
+  return SASGD_OK;
+}
 
 int sasgd_momentElements(const int64_t* numel, int32_t count, int64_t* out_elements) {
   if (!out_elements || count < 0 || (count > 0 && !numel)) return SASGD_EINVAL;
@@ -61,7 +169,7 @@ int sasgd_gradientNorm(const void* const* grads_dev, const int64_t* numel, int32
     if (numel[k] > 0 && (!grads_dev[k] || ((uintptr_t)grads_dev[k] & (bf ? 1 : 3)))) REFUSE("gradientNorm: tensor %d is null or not aligned to its elements", (int)k);
     blocks += blocks_of(numel[k]);
   }
-  if (blocks * kMomentBlock > kMostElements) REFUSE("gradientNorm: more than 2^38 elements");
+  if (blocks * kMomentBlock > kMostElements) REFUSE("gradientNorm: more than 2^35 elements");
   static_assert(kNormPartials * sizeof(double) <= SASGD_NORM_WORKSPACE, "partial sums do not fit the workspace");
   NormLaunch a;
   memset(&a, 0, sizeof(a));
@@ -131,7 +239,7 @@ int sasgd_applyAdamW(const sasgd_adamw* rule, const sasgd_tensor* tensors, int32
     has_shadow = has_shadow || t.shadow_out;
     blocks += blocks_of(t.numel);
   }
-  if (blocks * kMomentBlock > kMostElements) REFUSE("applyAdamW: more than 2^38 elements");
+  if (blocks * kMomentBlock > kMostElements) REFUSE("applyAdamW: more than 2^35 elements");
   if (blocks == 0) return SASGD_OK;
   if (!moments->m || !moments->v || (((uintptr_t)moments->m | (uintptr_t)moments->v) & 15)) REFUSE("applyAdamW: moments must be 16-byte aligned device pointers");
   if (e4m3 && (!moments->m_scale || !moments->v_scale || (((uintptr_t)moments->m_scale | (uintptr_t)moments->v_scale) & 3)))

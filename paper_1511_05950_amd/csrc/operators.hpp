@@ -52,4 +52,39 @@ int norm_grid(int64_t blocks);
 hipError_t launch_norm_partials(const NormLaunch& a, bool bf16, hipStream_t stream);
 hipError_t launch_norm_finish(const NormLaunch& a, hipStream_t stream);
 
+// ---------------------------------------------------------------- group normalisation (group_norm.hip)
+// How a call is cut into workgroups (group_norm_plan).
+struct GroupNormPlan {
+  int vec;         // channels a lane moves at a time: 16 bytes, or 1
+  int threads;
+  int held;        // vectors of x (and of dy) that a lane keeps in registers
+  bool whole;      // a workgroup holds all positions of `slab` channels; otherwise `chunk` positions of all channels, and a second launch
+  int slab, slabs;
+  int chunk, chunks;
+};
+struct GroupNormShape {
+  int64_t images;            // of a learner
+  int positions, channels, groups;
+  bool bf16;
+};
+GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient, int learners);
+
+// Addresses are base[learner] + a byte offset (workspace), wts[learner] + offset (scale, shift), grads[learner] + offset (their gradients);
+// context-free calls have one learner whose bases are 0.
+struct GroupNormArgs {
+  uintptr_t base[64], wts[64], grads[64];
+  int64_t x, y, dy, dx, stats, parts, sums;                 // parts: [image][chunk][group][2], sums: [image][chunk][channel][2], both fp32
+  int64_t scale, shift, dscale, dshift;
+  int64_t x_image, x_pixel, y_image, y_pixel;               // elements
+  GroupNormShape s;
+  GroupNormPlan plan;
+  int32_t learners, activation;
+  int32_t has_scale, has_shift, param_bf16, has_stats, has_dx, has_dscale, has_dshift, mask;   // mask: dx is 0 where x is not positive
+  float eps;
+};
+size_t group_norm_part_bytes(const GroupNormShape& s, const GroupNormPlan& p);
+size_t group_norm_sum_bytes(const GroupNormShape& s, const GroupNormPlan& p);
+hipError_t launch_group_norm(const GroupNormArgs& a, hipStream_t stream);
+hipError_t launch_group_norm_gradient(const GroupNormArgs& a, hipStream_t stream);
+
 }  // namespace sasgd
