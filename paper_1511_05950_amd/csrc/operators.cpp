@@ -81,7 +81,7 @@ const char* group_norm_args(const sasgd_norm_shape* shape, const void* x, const 
   const bool wide = (low & 15) == 0 && (a.s.channels | a.x_pixel | a.y_pixel | a.x_image | a.y_image) % vec == 0;
   if (!wide && a.s.channels > kNarrowChannels) return "more than 1024 channels must be whole 16 bytes, in strides and pointers too";
   a.plan = group_norm_plan(a.s, wide, gradient, 1);
-  if (a.s.images * (int64_t)(a.plan.whole ? a.plan.slabs : a.plan.chunks) * a.plan.threads >= ((int64_t)1 << 32)) return "too many images for a launch";
+  if ((a.s.images + 8) * (int64_t)(a.plan.whole ? a.plan.slabs : a.plan.chunks) * a.plan.threads >= ((int64_t)1 << 32)) return "too many images for a launch";
   const size_t need = need_bytes(a.s, a.plan, gradient);
   if (need > 0 && (!work || ((uintptr_t)work & 15) || work_bytes < need)) return "workspace missing, too small or not 16-byte aligned";
   a.x = (int64_t)(uintptr_t)x;

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "fastdiv.hpp"
+
 namespace sasgd {
 
 // ---------------------------------------------------------------- many tensors (adamw.hip)
@@ -58,7 +60,7 @@ struct GroupNormPlan {
   int vec;         // channels a lane moves at a time: 16 bytes, or 1
   int threads;
   int held;        // vectors of x (and of dy) that a lane keeps in registers
-  bool whole;      // a workgroup holds all positions of `slab` channels; otherwise `chunk` positions of all channels, and a second launch
+  bool whole;      // a workgroup holds all positions of `slab` channels; otherwise it walks `chunk` positions of all channels, in two launches
   int slab, slabs;
   int chunk, chunks;
 };
@@ -68,6 +70,13 @@ struct GroupNormShape {
   bool bf16;
 };
 GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient, int learners);
+
+// How a workgroup's lanes lie over a pixel's channels: `cols` vectors side by side, `rows` pixels at a time; n = cols x vec channels.
+struct GroupNormCols {
+  int cols, rows, segs;      // segs: lanes over n
+  int fold;                  // n is a power of two below 64
+  FastDiv by_cols, by_n;     // of numbers up to 1024: exact
+};
 
 // Addresses are base[learner] + a byte offset (workspace), wts[learner] + offset (scale, shift), grads[learner] + offset (their gradients);
 // context-free calls have one learner whose bases are 0.
@@ -81,10 +90,14 @@ struct GroupNormArgs {
   int32_t learners, activation;
   int32_t has_scale, has_shift, param_bf16, has_stats, has_dx, has_dscale, has_dshift, mask;   // mask: dx is 0 where x is not positive
   float eps;
+  // set by the launch
+  GroupNormCols cols[2];
+  int32_t cpg;               // channels of a group
+  FastDiv by_cpg;            // of channel numbers, up to 4096: exact
 };
 size_t group_norm_part_bytes(const GroupNormShape& s, const GroupNormPlan& p);
 size_t group_norm_sum_bytes(const GroupNormShape& s, const GroupNormPlan& p);
-hipError_t launch_group_norm(const GroupNormArgs& a, hipStream_t stream);
-hipError_t launch_group_norm_gradient(const GroupNormArgs& a, hipStream_t stream);
+hipError_t launch_group_norm(GroupNormArgs& a, hipStream_t stream);
+hipError_t launch_group_norm_gradient(GroupNormArgs& a, hipStream_t stream);
 
 }  // namespace sasgd
