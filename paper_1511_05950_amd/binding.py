@@ -336,24 +336,23 @@ def applyUpdateNoAlloc(theta_in_dev, theta_out_dev, v_dev, grads_dev, staleness,
                                        LR_MODES[lr_mode] if isinstance(lr_mode, str) else lr_mode, alpha0, momentum, weight_decay, stream)
 
 
-def _type(dtype):
-    """SASGD_FP32 or SASGD_BF16 of a torch type."""
-    name = str(dtype)
-    if name == "torch.float32":
-        return FP32
-    if name == "torch.bfloat16":
-        return BF16
-    raise TypeError("float32 or bfloat16 tensors are needed, not " + name)
-
-
-def _device():
+def _place(stream):
+    """(number of the current device, handle of the stream: the given one or torch's current one)."""
     import torch
-    return torch.cuda.current_device()
+    if not _fast_knows_torch:
+        load()
+        _fast.set_tensor_class(torch.Tensor, torch.float32, torch.bfloat16)
+        _fast_knows_torch.append(True)
+    device = torch.cuda.current_device()
+    return device, current_stream() if stream is None else stream
+
+
+_fast_knows_torch = []
 
 
 def _want(name, t, types, numel=None):
     """A contiguous tensor of one of the types (their names) on the current device, of at least `numel` elements where that is given."""
-    if t.get_device() != _device():
+    if t.get_device() != _place(0)[0]:
         raise ValueError(name + " is not on the current device")
     if str(t.dtype)[6:] not in types:
         raise TypeError("%s must be %s, not %s" % (name, " or ".join(types), t.dtype))
@@ -363,65 +362,10 @@ def _want(name, t, types, numel=None):
         raise ValueError("%s has %d elements, %d are needed" % (name, t.numel(), numel))
 
 
-def _want_bytes(call, t, size):
-    if t is None or t.numel() * t.element_size() < size or not t.is_contiguous() or t.get_device() != _device():
-        raise ValueError("%s needs a workspace of %d bytes on the current device" % (call, size))
-
-
-def _pixels(name, t):
-    """(images, positions, channels, image stride, pixel stride) of a tensor [images][height][width][channels] (or without width, or
-    without both): channels side by side, positions evenly apart."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) < 2:
-        raise ValueError(name + " must be [images, ..., channels]")
-    c = shape[-1]
-    positions, pixel = 1, c
-    if c > 1 and stride[-1] != 1:
-        raise ValueError(name + ": channels must be the last dimension, side by side")
-    for n, s in zip(reversed(shape[1:-1]), reversed(stride[1:-1])):
-        if n == 1:
-            continue
-        if positions == 1:
-            pixel = s
-        elif s != pixel * positions:
-            raise ValueError(name + ": positions must be evenly apart")
-        positions *= n
-    return shape[0], positions, c, stride[0] if shape[0] > 1 else pixel * positions, pixel
-
-
-def _norm_shape(x, y, groups, scale, activation, eps):
-    n, p, c, xi, xp = _pixels("x", x)
-    yi, yp = 0, 0
-    if y is not None:
-        if y.shape != x.shape or y.dtype is not x.dtype:
-            raise ValueError("x, y and the gradients must have one shape and one type")
-        _, _, _, yi, yp = _pixels("y", y)
-    return SasgdNormShape(n, p, c, groups, _type(x.dtype), FP32 if scale is None else _type(scale.dtype),
-                          ACTIVATIONS[activation] if isinstance(activation, str) else activation, eps, xi, xp, yi, yp)
-
-
-def _norm_tensors(x, scale, shift, stats, groups, *others):
-    device = _device()
-    for name, t in (("scale", scale), ("shift", shift)):
-        if t is not None:
-            if t.numel() != x.shape[-1] or not t.is_contiguous():
-                raise ValueError(name + " must have one value per channel")
-            if scale is not None and t.dtype is not scale.dtype or scale is None and str(t.dtype) != "torch.float32":
-                raise TypeError("scale and shift must have one type, a shift alone float32")
-    if stats is not None:
-        _want("stats", stats, ("float32",), 2 * x.shape[0] * groups)
-    for t in (x, scale, shift) + others:
-        if t is not None and t.get_device() != device:
-            raise ValueError("a tensor is not on the current device")
-
-
 def groupNormWorkspace(x, groups, gradient=False):
     """Bytes of workspace that groupNorm (groupNormGradient) needs for x [images, height, width, channels]."""
-    out = ctypes.c_size_t()
-    rc = load().sasgd_groupNormWorkspace(ctypes.byref(_norm_shape(x, None, groups, None, 0, 1e-5)), 1 if gradient else 0, ctypes.byref(out))
-    if rc != OK:
-        raise SasgdError(rc, "groupNormWorkspace: bad shape")
-    return out.value
+    _place(0)
+    return _fast.group_norm_workspace(x, groups, 1 if gradient else 0)
 
 
 def groupNorm(x, scale, shift, groups, y, stats=None, activation="none", eps=1e-5, workspace=None, stream=None):
@@ -429,45 +373,23 @@ def groupNorm(x, scale, shift, groups, y, stats=None, activation="none", eps=1e-
     include/sasgd.h).  x, y: float32 or bfloat16, channels side by side, pixels evenly apart (a slice of a wider tensor's channels will do);
     scale, shift: a value per channel, or None; stats: float32 [images, groups, 2] for the backward pass, or None; workspace:
     groupNormWorkspace bytes (None where that is 0)."""
-    lib = load()
-    _norm_tensors(x, scale, shift, stats, groups, y, workspace)
-    err = ctypes.create_string_buffer(256)
-    rc = lib.sasgd_groupNorm(ctypes.byref(_norm_shape(x, y, groups, scale if scale is not None else shift, activation, eps)), x.data_ptr(), _addr(scale), _addr(shift), y.data_ptr(),
-                             _addr(stats), _addr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                             current_stream() if stream is None else stream, err, 256)
-    if rc != OK:
-        raise SasgdError(rc, err.value.decode())
+    device, stream = _place(stream)
+    _fast.group_norm(x, scale, shift, groups, y, stats, ACTIVATIONS.get(activation, activation), eps, workspace, device, stream)
 
 
 def groupNormGradient(x, scale, shift, groups, stats, dy, dx=None, dscale=None, dshift=None, activation="none", workspace=None, stream=None):
     """sasgd_groupNormGradient: dx, dscale and dshift (each optional) of groupNorm's inputs from its output's gradient dy and the
     statistics it has kept.  dx has the strides of dy."""
-    lib = load()
-    _norm_tensors(x, scale, shift, stats, groups, dy, dx, dscale, dshift, workspace)
-    shape = _norm_shape(x, dy, groups, scale if scale is not None else shift, activation, 1e-5)
-    if dx is not None and (dx.shape != x.shape or dx.dtype is not x.dtype or _pixels("dx", dx) != _pixels("dy", dy)):
-        raise ValueError("dx must have the shape, type and strides of dy")
-    for name, t in (("dscale", dscale), ("dshift", dshift)):
-        if t is not None:
-            _want(name, t, ("float32",), x.shape[-1])
-    err = ctypes.create_string_buffer(256)
-    rc = lib.sasgd_groupNormGradient(ctypes.byref(shape), x.data_ptr(), _addr(scale), _addr(shift), stats.data_ptr(), dy.data_ptr(), _addr(dx), _addr(dscale),
-                                     _addr(dshift), _addr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                     current_stream() if stream is None else stream, err, 256)
-    if rc != OK:
-        raise SasgdError(rc, err.value.decode())
+    device, stream = _place(stream)
+    _fast.group_norm_gradient(x, scale, shift, groups, stats, dy, dx, dscale, dshift, ACTIVATIONS.get(activation, activation), workspace, device, stream)
 
 
 def gradientNorm(grads, out, max_norm=0.0, workspace=None, stream=None):
     """sasgd_gradientNorm: out[0] = the norm over all tensors of the list, out[1] = the factor that bounds it by max_norm (see
     include/sasgd.h).  grads: contiguous tensors of one type, float32 or bfloat16; out: float32 of two elements; workspace:
     NORM_WORKSPACE bytes of device memory."""
-    load()
-    dtype = grads[0].dtype if len(grads) else None
-    _want("out", out, ("float32",), 2)
-    _want_bytes("gradientNorm", workspace, NORM_WORKSPACE)
-    _fast.gradient_norm(grads, dtype, FP32 if dtype is None else _type(dtype), max_norm, out, workspace, _device(),
-                        current_stream() if stream is None else stream)
+    device, stream = _place(stream)
+    _fast.gradient_norm(grads, max_norm, out, workspace, device, stream)
 
 
 def momentElements(weights):
@@ -527,15 +449,11 @@ class AdamW:
         """One step.  grads: c lists of a gradient per tensor, contiguous and of one type, float32 or bfloat16; staleness: one per list
         (0 if not given); step: 1 in the first step (step_dev: a device int64 tensor that holds it instead); scale: device float, the
         factor of gradientNorm (its out[1:])."""
-        dtype = grads[0][0].dtype if len(grads) and len(grads[0]) else None
-        if dtype is not None:
-            self._rule.grad_type = _type(dtype)
-        if scale is not None:
-            _want("scale", scale, ("float32",), 1)
+        device, stream = _place(stream)
         if step_dev is not None:
             _want("step_dev", step_dev, ("int64",), 1)
-        _fast.apply_adamw(self._at[0], self._at[1], self._count, self._at[2], grads, dtype, [0] * len(grads) if staleness is None else staleness,
-                          step, step_dev, scale, _device(), current_stream() if stream is None else stream)
+        _fast.apply_adamw(self._at[0], self._at[1], self._count, self._at[2], grads, [0] * len(grads) if staleness is None else staleness, step, step_dev,
+                          scale, device, stream)
 
 
 def current_stream():

@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
@@ -60,7 +61,8 @@ def build(force=True, verbose=False):
 
 def build_pyext():
     """The CPython module of the per-gradient and per-update calls (host code only), linked against libsasgd.so beside it."""
-    cmd = [os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"], PYEXT_SRC, "-o", PYEXT,
+    torch = os.path.join(os.path.dirname(importlib.util.find_spec("torch").origin), "include")
+    cmd = [os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"], "-I", torch, PYEXT_SRC, "-o", PYEXT,
            "-L", HERE, "-l:libsasgd.so", "-Wl,-rpath,$ORIGIN"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

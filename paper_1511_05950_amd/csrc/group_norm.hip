@@ -82,6 +82,8 @@ __device__ __forceinline__ float param(const GroupNormArgs& A, uintptr_t at, int
   return A.param_bf16 ? bf2f(((const bf16_t*)at)[c]) : ((const float*)at)[c];
 }
 
+constexpr int kLaneChannels = 64;    // channels of a group up to which one lane adds them
+
 // Which image of a learner, and which slab of its channels or chunk of its positions, a workgroup works on.  Parts of one image are eight
 // workgroups apart: they run on one XCD at about the same time, where narrow slabs share the lines of L2.
 struct Place {
@@ -113,6 +115,14 @@ __device__ __forceinline__ Lanes lanes_of(const GroupNormCols& c, int t) {
   l.col = t - l.row * c.cols;
   l.active = l.row < c.rows;
   return l;
+}
+
+// Sum over the wavefront, in every lane: shifts within rows of 16 lanes, then rows to rows, without a trip through LDS.
+__device__ __forceinline__ float wave_total(float v) {
+#define STEP(ctrl, rows) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xf, true));
+  STEP(0x111, 0xf) STEP(0x112, 0xf) STEP(0x114, 0xf) STEP(0x118, 0xf) STEP(0x142, 0xa) STEP(0x143, 0xc)
+#undef STEP
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 // Sums over the rows of lanes, channel by channel (n = cols V of them), of K quantities at a time; lane (seg, c) adds the rows
@@ -188,20 +198,36 @@ __device__ __forceinline__ void channel_moments(const float (&sum)[V], const flo
   });
 }
 
-// Group g of the workgroup's channels from their moments, by a wavefront: mean and sum of squared distances of its cpg np values.
-__device__ __forceinline__ float2 group_moments(const float* mean, const float* m2, int g, int cpg, int np, int lane) {
-  float s = 0.f, d = 0.f;
-  for (int c = lane; c < cpg; c += 64) {
-    s += mean[g * cpg + c];
-    d += m2[g * cpg + c];
+// The workgroup's groups from the moments of their channels (mean[c], m2[c] of `np` values each): done(g, mean, sum of squared distances).  A lane a
+// group, or a wavefront a group where they have many channels (320 channels in 32 groups by wavefronts: 4 us of a workgroup's 9).
+template <typename F>
+__device__ __forceinline__ void group_moments(const float* mean, const float* m2, int groups, int cpg, int np, F done) {
+  const int t = threadIdx.x, T = blockDim.x;
+  if (cpg <= kLaneChannels) {
+    for (int g = t; g < groups; g += T) {
+      float s = 0.f, d = 0.f, off = 0.f;
+      for (int c = g * cpg; c < (g + 1) * cpg; c++) {
+        s += mean[c];
+        d += m2[c];
+      }
+      const float mu = s / (float)cpg;
+      for (int c = g * cpg; c < (g + 1) * cpg; c++) off += (mean[c] - mu) * (mean[c] - mu);
+      done(g, mu, d + (float)np * off);
+    }
+    return;
   }
-  const float mu = wave_sum(s) / (float)cpg;
-  float off = 0.f;
-  for (int c = lane; c < cpg; c += 64) {
-    const float e = mean[g * cpg + c] - mu;
-    off += e * e;
+  const int lane = t & 63;
+  for (int g = t >> 6; g < groups; g += T >> 6) {
+    float s = 0.f, d = 0.f, off = 0.f;
+    for (int c = g * cpg + lane; c < (g + 1) * cpg; c += 64) {
+      s += mean[c];
+      d += m2[c];
+    }
+    const float mu = wave_total(s) / (float)cpg;
+    for (int c = g * cpg + lane; c < (g + 1) * cpg; c += 64) off += (mean[c] - mu) * (mean[c] - mu);
+    const float m = wave_total(d) + (float)np * wave_total(off);
+    if (lane == 0) done(g, mu, m);
   }
-  return make_float2(mu, wave_sum(d) + (float)np * wave_sum(off));
 }
 
 template <typename T, int V>
@@ -271,16 +297,12 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
     close_moments<V>(first, s, q, count);
     channel_moments<V>(s, q, cols, l, np, rows, red, mean, m2);
   }
-  const int lane = t & 63, gs = A.by_cpg(S);
-  for (int g = t >> 6; g < gs; g += threads >> 6) {
-    const float2 mom = group_moments(mean, m2, g, cpg, np, lane);
-    if (lane == 0) {
-      const float r = 1.f / sqrtf(mom.y / ((float)np * (float)cpg) + A.eps);
-      group[2 * g] = mom.x;
-      group[2 * g + 1] = r;
-      if (A.has_stats) ((float2*)(base + A.stats))[at.image * A.s.groups + A.by_cpg(c0) + g] = make_float2(mom.x, r);
-    }
-  }
+  group_moments(mean, m2, A.by_cpg(S), cpg, np, [&](int g, float mu, float sq) {
+    const float r = 1.f / sqrtf(sq / ((float)np * (float)cpg) + A.eps);
+    group[2 * g] = mu;
+    group[2 * g + 1] = r;
+    if (A.has_stats) ((float2*)(base + A.stats))[at.image * A.s.groups + A.by_cpg(c0) + g] = make_float2(mu, r);
+  });
   __syncthreads();
   if (count == 0) return;
   float mu[V], r[V], slope[V];
@@ -344,14 +366,11 @@ __global__ __launch_bounds__(256) void group_norm_chunk_kernel(const GroupNormAr
     close_moments<V>(first, s, q, count);
     channel_moments<V>(s, q, cols, l, np, rows, red, mean + c0, m2 + c0);
   }
-  const int lane = t & 63;
-  for (int g = t >> 6; g < A.s.groups; g += threads >> 6) {
-    const float2 mom = group_moments(mean, m2, g, cpg, np, lane);
-    if (lane == 0) ((float2*)(base + A.parts))[(at.image * A.plan.chunks + at.part) * A.s.groups + g] = mom;
-  }
+  float2* parts = (float2*)(base + A.parts) + (at.image * A.plan.chunks + at.part) * A.s.groups;
+  group_moments(mean, m2, A.s.groups, cpg, np, [&](int g, float mu, float sq) { parts[g] = make_float2(mu, sq); });
 }
 
-// Second launch: the image's statistics from its chunks', then y.  LDS: group [2 groups], parts [2 groups chunks]
+// Second launch: the image's statistics from its chunks', then y.  LDS: group [2 groups]
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(256) void group_norm_apply_kernel(const GroupNormArgs A) {
   extern __shared__ float group[];
@@ -362,22 +381,25 @@ __global__ __launch_bounds__(256) void group_norm_apply_kernel(const GroupNormAr
   const int C = A.s.channels, G = A.s.groups, chunk = A.plan.chunk, chunks = A.plan.chunks;
   const int p0 = at.part * chunk, np = min(chunk, A.s.positions - p0);
   const int t = threadIdx.x, threads = blockDim.x;
-  float2* parts = (float2*)(group + 2 * G);
-  for (int i = t; i < chunks * G; i += threads) parts[i] = ((const float2*)(base + A.parts))[at.image * chunks * G + i];
-  __syncthreads();
+  const float2* parts = (const float2*)(base + A.parts) + at.image * chunks * G;
   const float last = (float)(A.s.positions - (chunks - 1) * chunk), full = (float)chunk, total = (float)A.s.positions, cpg = (float)A.cpg;
-  for (int g = t; g < G; g += threads) {
+  for (int i = t; i < G * A.spread; i += threads) {          // `spread` neighbouring lanes a group
+    const int g = i / A.spread, first = i - g * A.spread;
     float s = 0.f, m2 = 0.f;
-    for (int k = 0; k < chunks; k++) s += parts[k * G + g].x * (k < chunks - 1 ? full : last);
+    for (int k = first; k < chunks; k += A.spread) s += parts[k * G + g].x * (k < chunks - 1 ? full : last);
+    for (int o = 1; o < A.spread; o <<= 1) s += __shfl_xor(s, o, 64);
     const float mu = s / total;
-    for (int k = 0; k < chunks; k++) {
+    for (int k = first; k < chunks; k += A.spread) {
       const float2 p = parts[k * G + g];
       m2 += p.y + (k < chunks - 1 ? full : last) * cpg * (p.x - mu) * (p.x - mu);
     }
-    const float r = 1.f / sqrtf(m2 / (total * cpg) + A.eps);
-    group[2 * g] = mu;
-    group[2 * g + 1] = r;
-    if (A.has_stats && at.part == 0) ((float2*)(base + A.stats))[at.image * G + g] = make_float2(mu, r);
+    for (int o = 1; o < A.spread; o <<= 1) m2 += __shfl_xor(m2, o, 64);
+    if (first == 0) {
+      const float r = 1.f / sqrtf(m2 / (total * cpg) + A.eps);
+      group[2 * g] = mu;
+      group[2 * g + 1] = r;
+      if (A.has_stats && at.part == 0) ((float2*)(base + A.stats))[at.image * G + g] = make_float2(mu, r);
+    }
   }
   __syncthreads();
   for (int c0 = 0; c0 < C; c0 += A.cols[0].cols * V) {
@@ -467,15 +489,34 @@ __device__ __forceinline__ void gradient_sums(const float (&a)[V], const float (
   row_sums<2>(cols, n, red, out, stride, [&](int k, int r, int c) { return (k ? rb : rows)[r * n + c]; });
 }
 
-// s1 and s2 of group g of the workgroup's channels (the first is channel c0 of the image), by a wavefront
-__device__ __forceinline__ float2 group_gradient(const GroupNormArgs& A, uintptr_t wts, const float* sa, const float* sb, int c0, int g, int lane) {
-  float s1 = 0.f, s2 = 0.f;
-  for (int c = g * A.cpg + lane; c < (g + 1) * A.cpg; c += 64) {
-    const float w = A.has_scale ? param(A, wts + A.scale, c0 + c) : 1.f;
-    s1 = fmaf(w, sa[c], s1);
-    s2 = fmaf(w, sb[c], s2);
+// s1 and s2 of the workgroup's groups from its channels' sums (the first is channel c0 of the image): done(g, s1, s2)
+template <typename F>
+__device__ __forceinline__ void group_gradient(const GroupNormArgs& A, uintptr_t wts, const float* sa, const float* sb, int c0, int groups, F done) {
+  const int t = threadIdx.x, T = blockDim.x, cpg = A.cpg;
+  if (cpg <= kLaneChannels) {
+    for (int g = t; g < groups; g += T) {
+      float s1 = 0.f, s2 = 0.f;
+      for (int c = g * cpg; c < (g + 1) * cpg; c++) {
+        const float w = A.has_scale ? param(A, wts + A.scale, c0 + c) : 1.f;
+        s1 = fmaf(w, sa[c], s1);
+        s2 = fmaf(w, sb[c], s2);
+      }
+      done(g, s1, s2);
+    }
+    return;
   }
-  return make_float2(wave_sum(s1), wave_sum(s2));
+  const int lane = t & 63;
+  for (int g = t >> 6; g < groups; g += T >> 6) {
+    float s1 = 0.f, s2 = 0.f;
+    for (int c = g * cpg + lane; c < (g + 1) * cpg; c += 64) {
+      const float w = A.has_scale ? param(A, wts + A.scale, c0 + c) : 1.f;
+      s1 = fmaf(w, sa[c], s1);
+      s2 = fmaf(w, sb[c], s2);
+    }
+    s1 = wave_total(s1);
+    s2 = wave_total(s2);
+    if (lane == 0) done(g, s1, s2);
+  }
 }
 
 // What a lane keeps of dy between the sums and dx: dz.  Behind a ReLU or nothing that is dy or 0 and stays in its type, behind silu fp32.
@@ -552,14 +593,10 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
     for (int c = t; c < S; c += threads) out[c] = make_float2(sums[S + c], sums[c]);
   }
   if (!A.has_dx) return;
-  const int lane = t & 63, gs = A.by_cpg(S);
-  for (int g = t >> 6; g < gs; g += threads >> 6) {
-    const float2 s = group_gradient(A, wts, sums, sums + S, c0, g, lane);
-    if (lane == 0) {
-      group[2 * g] = s.x;
-      group[2 * g + 1] = s.y;
-    }
-  }
+  group_gradient(A, wts, sums, sums + S, c0, A.by_cpg(S), [&](int g, float s1, float s2) {
+    group[2 * g] = s1;
+    group[2 * g + 1] = s2;
+  });
   __syncthreads();
   if (count == 0) return;
   const float inv = 1.f / ((float)np * (float)A.cpg);
@@ -638,14 +675,11 @@ __global__ __launch_bounds__(256) void group_norm_gradient_chunk_kernel(const Gr
   float2* out = (float2*)(base + A.sums) + (at.image * A.plan.chunks + at.part) * C;
   for (int c = t; c < C; c += threads) out[c] = make_float2(sb[c], sa[c]);
   if (!A.has_dx) return;
-  const int lane = t & 63;
-  for (int g = t >> 6; g < A.s.groups; g += threads >> 6) {
-    const float2 s = group_gradient(A, wts, sa, sb, 0, g, lane);
-    if (lane == 0) ((float2*)(base + A.parts))[(at.image * A.plan.chunks + at.part) * A.s.groups + g] = s;
-  }
+  float2* parts = (float2*)(base + A.parts) + (at.image * A.plan.chunks + at.part) * A.s.groups;
+  group_gradient(A, wts, sa, sb, 0, A.s.groups, [&](int g, float s1, float s2) { parts[g] = make_float2(s1, s2); });
 }
 
-// Second launch: s1 and s2 of the image from its chunks', then dx.  LDS: group [2 groups], parts [2 groups chunks]
+// Second launch: s1 and s2 of the image from its chunks', then dx.  LDS: group [2 groups]
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(256) void group_norm_gradient_apply_kernel(const GroupNormArgs A) {
   extern __shared__ float group[];
@@ -656,18 +690,23 @@ __global__ __launch_bounds__(256) void group_norm_gradient_apply_kernel(const Gr
   const int C = A.s.channels, G = A.s.groups, chunks = A.plan.chunks;
   const int p0 = at.part * A.plan.chunk, np = min(A.plan.chunk, A.s.positions - p0);
   const int t = threadIdx.x, threads = blockDim.x;
-  float2* parts = (float2*)(group + 2 * G);
-  for (int i = t; i < chunks * G; i += threads) parts[i] = ((const float2*)(base + A.parts))[at.image * chunks * G + i];
-  __syncthreads();
+  const float2* parts = (const float2*)(base + A.parts) + at.image * chunks * G;
   const float inv = 1.f / ((float)A.s.positions * (float)A.cpg);
-  for (int g = t; g < G; g += threads) {
+  for (int i = t; i < G * A.spread; i += threads) {
+    const int g = i / A.spread, first = i - g * A.spread;
     float s1 = 0.f, s2 = 0.f;
-    for (int k = 0; k < chunks; k++) {
+    for (int k = first; k < chunks; k += A.spread) {
       s1 += parts[k * G + g].x;
       s2 += parts[k * G + g].y;
     }
-    group[2 * g] = s1 * inv;
-    group[2 * g + 1] = s2 * inv;
+    for (int o = 1; o < A.spread; o <<= 1) {
+      s1 += __shfl_xor(s1, o, 64);
+      s2 += __shfl_xor(s2, o, 64);
+    }
+    if (first == 0) {
+      group[2 * g] = s1 * inv;
+      group[2 * g + 1] = s2 * inv;
+    }
   }
   __syncthreads();
   for (int c0 = 0; c0 < C; c0 += A.cols[0].cols * V) {
@@ -816,7 +855,7 @@ GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient,
   // chunks of 64 KiB, smaller ones where that makes fewer than 1 024 workgroups, at most 32 an image and at least 16 KiB
   const int64_t image = (int64_t)s.positions * s.channels * size, images = std::max<int64_t>(1, s.images * learners);
   int64_t chunks = std::max((image + 65535) / 65536, (1024 + images - 1) / images);
-  chunks = std::min(std::min(chunks, image / 16384), std::min<int64_t>(32, 4096 / s.groups));     // (LDS of the second launch)
+  chunks = std::min(std::min(chunks, image / 16384), (int64_t)32);
   chunks = std::max<int64_t>(1, chunks);
   p.chunk = (int)((s.positions + chunks - 1) / chunks);
   p.chunks = (s.positions + p.chunk - 1) / p.chunk;
@@ -850,6 +889,7 @@ static void set_columns(GroupNormArgs& a) {
   }
   a.cpg = a.s.channels / a.s.groups;
   a.by_cpg.set(a.cpg);
+  for (a.spread = 1; a.spread < 64 && a.spread * 2 <= a.plan.chunks && a.spread * 2 * a.s.groups <= a.plan.threads;) a.spread *= 2;
 }
 
 #define BY_ACTIVATION(launch)                                                  \
@@ -888,7 +928,7 @@ static hipError_t forward(const GroupNormArgs& a, hipStream_t stream) {
   group_norm_chunk_kernel<T, V><<<grid, a.plan.threads, lds_bytes(a, false), stream>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  auto launch = [&](auto act) { group_norm_apply_kernel<T, V, decltype(act)::value><<<grid, a.plan.threads, (size_t)a.s.groups * (1 + a.plan.chunks) * 8, stream>>>(a); };
+  auto launch = [&](auto act) { group_norm_apply_kernel<T, V, decltype(act)::value><<<grid, a.plan.threads, (size_t)a.s.groups * 8, stream>>>(a); };
   BY_ACTIVATION(launch);
   return hipGetLastError();
 }
@@ -914,7 +954,7 @@ static hipError_t backward(const GroupNormArgs& a, hipStream_t stream) {
   BY_ACTIVATION(sums);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.has_dx) return e;
-  auto launch = [&](auto act) { group_norm_gradient_apply_kernel<T, V, decltype(act)::value><<<grid, a.plan.threads, (size_t)a.s.groups * (1 + a.plan.chunks) * 8, stream>>>(a); };
+  auto launch = [&](auto act) { group_norm_gradient_apply_kernel<T, V, decltype(act)::value><<<grid, a.plan.threads, (size_t)a.s.groups * 8, stream>>>(a); };
   BY_ACTIVATION(launch);
   return hipGetLastError();
 }

@@ -94,6 +94,7 @@ struct GroupNormArgs {
   GroupNormCols cols[2];
   int32_t cpg;               // channels of a group
   FastDiv by_cpg;            // of channel numbers, up to 4096: exact
+  int32_t spread;            // lanes that add one group's chunks in the second launch, a power of two
 };
 size_t group_norm_part_bytes(const GroupNormShape& s, const GroupNormPlan& p);
 size_t group_norm_sum_bytes(const GroupNormShape& s, const GroupNormPlan& p);

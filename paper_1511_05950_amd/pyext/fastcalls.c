@@ -6,6 +6,9 @@
 #include <Python.h>
 #include <stdint.h>
 #include <stdio.h>
+#include <string.h>
+
+#include <ATen/dlpack.h>               /* torch's tensors through their C interface */
 
 #include "../../include/sasgd.h"
 
@@ -14,8 +17,9 @@ static PyObject* s_data_ptr;      /* "data_ptr" */
 static PyObject* s_ctypes;        /* "ctypes" */
 static PyObject* s_data;          /* "data" */
 static PyObject* s_dtype;         /* "dtype" */
-static PyObject* s_numel;         /* "numel" */
-static PyObject* s_is_contiguous; /* "is_contiguous" */
+static PyObject* s_shape;         /* "shape" */
+static PyObject* s_stride;        /* "stride" */
+static PyObject* s_element_size;  /* "element_size" */
 static PyObject* s_get_device;    /* "get_device" */
 
 static PyObject* raise_code(int code, const char* msg) {
@@ -257,112 +261,206 @@ static PyObject* apply_update_no_alloc(PyObject* self, PyObject* const* a, Py_ss
   return PyLong_FromLong(rc);
 }
 
-/* One tensor of a list: its address, checked to be a contiguous tensor of `dtype` on device number `device`; its length into *numel, or
- * checked against it where that is not negative. */
-static int list_tensor(PyObject* o, PyObject* dtype, long device, int64_t* numel, void** out) {
-  PyObject* v;
-  long long n;
-  int same;
-  v = PyObject_CallMethodNoArgs(o, s_get_device);
-  if (!v) return -1;
-  n = PyLong_AsLongLong(v);
-  Py_DECREF(v);
-  if (n == -1 && PyErr_Occurred()) return -1;
-  if (n != device) {
-    PyErr_SetString(PyExc_ValueError, "a tensor is not on the current device");
-    return -1;
-  }
-  v = PyObject_GetAttr(o, s_dtype);
-  if (!v) return -1;
-  same = v == dtype;
-  Py_DECREF(v);
-  if (!same) {
-    PyErr_SetString(PyExc_TypeError, "tensors of another type than the first one's");
-    return -1;
-  }
-  v = PyObject_CallMethodNoArgs(o, s_is_contiguous);
-  if (!v) return -1;
-  same = v == Py_True;
-  Py_DECREF(v);
-  if (!same) {
-    PyErr_SetString(PyExc_ValueError, "a tensor is not contiguous");
-    return -1;
-  }
-  v = PyObject_CallMethodNoArgs(o, s_numel);
-  if (!v) return -1;
-  n = PyLong_AsLongLong(v);
-  Py_DECREF(v);
-  if (n == -1 && PyErr_Occurred()) return -1;
-  if (*numel >= 0 && n != *numel) {
-    PyErr_SetString(PyExc_ValueError, "a gradient's length is not its tensor's");
-    return -1;
-  }
-  *numel = n;
-  return address(o, out);
+/* A tensor as the calls below need it. */
+#define MOST_DIMS 8
+enum { KIND_OTHER = -1 };             /* else SASGD_FP32, SASGD_BF16 */
+typedef struct {
+  void* data;
+  int device, kind, dims, itemsize;
+  const int64_t *shape, *stride;       /* elements */
+  int64_t own[2 * MOST_DIMS];
+} view;
+
+static PyObject *tensor_class, *fp32_type, *bf16_type;      /* torch.Tensor, torch.float32, torch.bfloat16: set_tensor_class */
+static const DLPackExchangeAPI* exchange;                   /* torch's C interface to its tensors, where it has one: 20 ns a tensor instead of 200 */
+
+static int bad(PyObject* kind, const char* what, const char* why) {
+  PyErr_Format(kind, "%s %s", what, why);
+  return -1;
 }
 
-/* gradient_norm(grads, dtype, type, max_norm, out, workspace, device, stream) */
+static int tuple_of(PyObject* o, PyObject* name, int call, int64_t* out, int* dims) {
+  PyObject* t = call ? PyObject_CallMethodNoArgs(o, name) : PyObject_GetAttr(o, name);
+  Py_ssize_t k, n;
+  if (!t) return -1;
+  n = PyTuple_Check(t) ? PyTuple_GET_SIZE(t) : MOST_DIMS + 1;
+  if (n > MOST_DIMS) {
+    Py_DECREF(t);
+    return bad(PyExc_ValueError, "a tensor", "has too many dimensions");
+  }
+  for (k = 0; k < n; k++) out[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, k));
+  Py_DECREF(t);
+  *dims = (int)n;
+  return PyErr_Occurred() ? -1 : 0;
+}
+
+static int view_of(PyObject* o, view* v) {
+  PyObject* a;
+  if (exchange && (PyObject*)Py_TYPE(o) == tensor_class) {
+    DLTensor t;
+    if (exchange->dltensor_from_py_object_no_sync(o, &t) == 0 && t.ndim <= MOST_DIMS) {
+      int k;
+      int64_t n = 1;
+      v->data = (char*)t.data + t.byte_offset;
+      v->device = t.device.device_type == kDLCUDA || t.device.device_type == kDLROCM ? t.device.device_id : -1;
+      v->kind = t.dtype.lanes != 1 ? KIND_OTHER : t.dtype.code == kDLFloat && t.dtype.bits == 32 ? SASGD_FP32
+                : t.dtype.code == kDLBfloat && t.dtype.bits == 16 ? SASGD_BF16 : KIND_OTHER;
+      v->itemsize = (t.dtype.bits + 7) / 8;
+      v->dims = t.ndim;
+      v->shape = t.shape;
+      v->stride = t.strides;
+      if (!t.strides) {
+        for (k = t.ndim - 1; k >= 0; k--) {
+          v->own[k] = n;
+          n *= t.shape[k];
+        }
+        v->stride = v->own;
+      }
+      return 0;
+    }
+    PyErr_Clear();                     /* a kind of tensor that it does not show */
+  }
+  if (address(o, &v->data)) return -1;
+  a = PyObject_CallMethodNoArgs(o, s_get_device);
+  if (!a) return -1;
+  v->device = (int)PyLong_AsLong(a);
+  Py_DECREF(a);
+  a = PyObject_GetAttr(o, s_dtype);
+  if (!a) return -1;
+  v->kind = a == fp32_type ? SASGD_FP32 : a == bf16_type ? SASGD_BF16 : KIND_OTHER;
+  Py_DECREF(a);
+  a = PyObject_CallMethodNoArgs(o, s_element_size);
+  if (!a) return -1;
+  v->itemsize = (int)PyLong_AsLong(a);
+  Py_DECREF(a);
+  v->shape = v->own;
+  v->stride = v->own + MOST_DIMS;
+  return tuple_of(o, s_shape, 0, v->own, &v->dims) || tuple_of(o, s_stride, 1, v->own + MOST_DIMS, &v->dims) ? -1 : 0;
+}
+
+static int64_t elements(const view* v) {
+  int64_t n = 1;
+  int k;
+  for (k = 0; k < v->dims; k++) n *= v->shape[k];
+  return n;
+}
+static int contiguous(const view* v) {
+  int64_t n = 1;
+  int k;
+  for (k = v->dims - 1; k >= 0; k--) {
+    if (v->shape[k] != 1 && v->stride[k] != n && elements(v) > 0) return 0;
+    n *= v->shape[k];
+  }
+  return 1;
+}
+
+/* A contiguous tensor on the device, of `kind` where that is not KIND_OTHER, of at least `least` elements. */
+static int want(PyObject* o, const char* name, int device, int kind, int64_t least, view* v) {
+  if (view_of(o, v)) return -1;
+  if (v->device != device) return bad(PyExc_ValueError, name, "is not on the current device");
+  if (kind != KIND_OTHER && v->kind != kind) return bad(PyExc_TypeError, name, kind == SASGD_FP32 ? "must be float32" : "must be bfloat16");
+  if (!contiguous(v)) return bad(PyExc_ValueError, name, "must be contiguous");
+  if (elements(v) < least) return bad(PyExc_ValueError, name, "has too few elements");
+  return 0;
+}
+
+/* Bytes and address of a workspace (None: none). */
+static int workspace_of(PyObject* o, int device, void** data, size_t* bytes) {
+  view v;
+  *data = NULL;
+  *bytes = 0;
+  if (o == Py_None) return 0;
+  if (want(o, "workspace", device, KIND_OTHER, 0, &v)) return -1;
+  *data = v.data;
+  *bytes = (size_t)elements(&v) * (size_t)v.itemsize;
+  return 0;
+}
+
+/* The tensors of a list: contiguous, on the device, all of the first one's kind (*kind; SASGD_FP32 of an empty list).  numel: their lengths,
+ * written, or where `known` compared with. */
+static int list_of(PyObject* seq, Py_ssize_t n, int device, int* kind, const void** data, size_t apart, int64_t* numel, size_t numel_apart, int known) {
+  Py_ssize_t k;
+  for (k = 0; k < n; k++) {
+    view v;
+    int64_t count, *at = (int64_t*)((char*)numel + (size_t)k * numel_apart);
+    if (view_of(PySequence_Fast_GET_ITEM(seq, k), &v)) return -1;
+    if (v.device != device) return bad(PyExc_ValueError, "a gradient", "is not on the current device");
+    if (v.kind == KIND_OTHER) return bad(PyExc_TypeError, "a gradient", "must be float32 or bfloat16");
+    if (*kind == KIND_OTHER) *kind = v.kind;
+    if (v.kind != *kind) return bad(PyExc_TypeError, "a gradient", "has another type than the first one");
+    if (!contiguous(&v)) return bad(PyExc_ValueError, "a gradient", "must be contiguous");
+    count = elements(&v);
+    if (known && count != *at) return bad(PyExc_ValueError, "a gradient", "has not its tensor's length");
+    if (!known) *at = count;
+    data[(size_t)k * apart] = v.data;
+  }
+  return 0;
+}
+
+/* gradient_norm(grads, max_norm, out, workspace, device, stream) */
 static PyObject* gradient_norm(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
-  int32_t type, device;
+  int32_t device;
+  int kind = KIND_OTHER;
   double max_norm;
-  void *out, *work, *stream;
-  Py_ssize_t n, k;
+  void *work, *stream;
+  size_t bytes;
+  Py_ssize_t n;
   PyObject* seq;
   const void** grads;
   int64_t* numel;
+  view out;
   char err[256] = "";
-  int rc, bad = 0;
-  NARGS(8);
-  if (integer32(a[2], &type) || address(a[4], &out) || address(a[5], &work) || integer32(a[6], &device) || address(a[7], &stream)) return NULL;
-  max_norm = PyFloat_AsDouble(a[3]);
+  int rc = 0, failed;
+  NARGS(6);
+  max_norm = PyFloat_AsDouble(a[1]);
   if (PyErr_Occurred()) return NULL;
+  if (integer32(a[4], &device) || address(a[5], &stream) || want(a[2], "out", device, SASGD_FP32, 2, &out) || workspace_of(a[3], device, &work, &bytes)) return NULL;
+  if (bytes < SASGD_NORM_WORKSPACE) {
+    PyErr_Format(PyExc_ValueError, "gradientNorm needs a workspace of %d bytes", SASGD_NORM_WORKSPACE);
+    return NULL;
+  }
   seq = PySequence_Fast(a[0], "grads must be a sequence");
   if (!seq) return NULL;
   n = PySequence_Fast_GET_SIZE(seq);
-  if (n > INT32_MAX) {
-    Py_DECREF(seq);
-    return raise_code(SASGD_EINVAL, "gradientNorm: too many tensors");
-  }
   grads = (const void**)PyMem_Malloc(sizeof(void*) * (size_t)(n ? n : 1));
   numel = (int64_t*)PyMem_Malloc(sizeof(int64_t) * (size_t)(n ? n : 1));
-  bad = !grads || !numel;
-  if (bad) PyErr_NoMemory();
-  for (k = 0; !bad && k < n; k++) {
-    numel[k] = -1;
-    bad = list_tensor(PySequence_Fast_GET_ITEM(seq, k), a[1], device, &numel[k], (void**)&grads[k]);
-  }
+  failed = !grads || !numel || n > INT32_MAX;
+  if (failed) PyErr_NoMemory();
+  else failed = list_of(seq, n, device, &kind, grads, 1, numel, sizeof(int64_t), 0);
   Py_DECREF(seq);
-  rc = 0;
-  if (!bad) {
+  if (!failed) {
     Py_BEGIN_ALLOW_THREADS
-    rc = sasgd_gradientNorm(grads, numel, (int32_t)n, type, (float)max_norm, (float*)out, work, stream, err, sizeof(err));
+    rc = sasgd_gradientNorm(grads, numel, (int32_t)n, kind == KIND_OTHER ? SASGD_FP32 : kind, (float)max_norm, (float*)out.data, work, stream, err, sizeof(err));
     Py_END_ALLOW_THREADS
   }
   PyMem_Free(grads);
   PyMem_Free(numel);
-  if (bad) return NULL;
+  if (failed) return NULL;
   if (rc) return raise_code(rc, err);
   Py_RETURN_NONE;
 }
 
-/* apply_adamw(rule, tensors, count, moments, grads, dtype, staleness, step, step_dev, factor, device, stream): rule, tensors and moments are addresses
- * of the C structures, grads a sequence of c sequences of `count` tensors. */
+/* apply_adamw(rule, tensors, count, moments, grads, staleness, step, step_dev, factor, device, stream): rule, tensors and moments are addresses of the
+ * C structures, grads a sequence of c sequences of `count` tensors; the rule's grad_type becomes theirs. */
 static PyObject* apply_adamw(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
-  void *rule, *tensors, *moments, *step_dev, *factor, *stream;
+  void *rule, *tensors, *moments, *step_dev, *stream;
   int32_t count, device, stale[SASGD_NOALLOC_MAX_GRADIENTS];
+  int kind = KIND_OTHER, rc = 0, failed = 0;
   long long step;
-  Py_ssize_t c, l, k;
+  Py_ssize_t c, l;
   PyObject *lists, *st;
-  const void** grads = NULL;
+  const void** grads;
+  view factor;
   char err[256] = "";
-  int rc = 0, bad = 0;
-  NARGS(12);
-  if (address(a[0], &rule) || address(a[1], &tensors) || integer32(a[2], &count) || address(a[3], &moments) || integer(a[7], &step) ||
-      address(a[8], &step_dev) || address(a[9], &factor) || integer32(a[10], &device) || address(a[11], &stream))
+  NARGS(11);
+  if (address(a[0], &rule) || address(a[1], &tensors) || integer32(a[2], &count) || address(a[3], &moments) || integer(a[6], &step) ||
+      address(a[7], &step_dev) || integer32(a[9], &device) || address(a[10], &stream))
     return NULL;
+  factor.data = NULL;
+  if (a[8] != Py_None && want(a[8], "scale", device, SASGD_FP32, 1, &factor)) return NULL;
   lists = PySequence_Fast(a[4], "grads must be a sequence of sequences");
   if (!lists) return NULL;
-  st = PySequence_Fast(a[6], "staleness must be a sequence");
+  st = PySequence_Fast(a[5], "staleness must be a sequence");
   if (!st) {
     Py_DECREF(lists);
     return NULL;
@@ -373,41 +471,195 @@ static PyObject* apply_adamw(PyObject* self, PyObject* const* a, Py_ssize_t narg
     Py_DECREF(st);
     return raise_code(SASGD_EINVAL, "applyAdamW: 1..64 gradients and as many staleness values are needed");
   }
-  for (l = 0; !bad && l < c; l++) bad = as_integer32(PySequence_Fast_GET_ITEM(st, l), &stale[l]);
+  for (l = 0; !failed && l < c; l++) failed = as_integer32(PySequence_Fast_GET_ITEM(st, l), &stale[l]);
   Py_DECREF(st);
-  if (!bad) {
-    grads = (const void**)PyMem_Malloc(sizeof(void*) * (size_t)(count > 0 ? count : 1) * (size_t)c);
-    if (!grads) {
-      PyErr_NoMemory();
-      bad = 1;
-    }
+  grads = failed ? NULL : (const void**)PyMem_Malloc(sizeof(void*) * (size_t)(count > 0 ? count : 1) * (size_t)c);
+  if (!failed && !grads) {
+    PyErr_NoMemory();
+    failed = 1;
   }
-  for (l = 0; !bad && l < c; l++) {
+  for (l = 0; !failed && l < c; l++) {
     PyObject* one = PySequence_Fast(PySequence_Fast_GET_ITEM(lists, l), "grads must be a sequence of sequences");
     if (!one) {
-      bad = 1;
+      failed = 1;
       break;
     }
     if (PySequence_Fast_GET_SIZE(one) != count) {
       PyErr_SetString(PyExc_ValueError, "a gradient has another number of tensors than the weights");
-      bad = 1;
-    }
-    for (k = 0; !bad && k < count; k++) {
-      int64_t numel = ((const sasgd_tensor*)tensors)[k].numel;
-      bad = list_tensor(PySequence_Fast_GET_ITEM(one, k), a[5], device, &numel, (void**)&grads[k * c + l]);
+      failed = 1;
+    } else {
+      failed = list_of(one, count, device, &kind, grads + l, (size_t)c, &((sasgd_tensor*)tensors)->numel, sizeof(sasgd_tensor), 1);
     }
     Py_DECREF(one);
   }
   Py_DECREF(lists);
-  if (!bad) {
+  if (!failed) {
+    if (kind != KIND_OTHER) ((sasgd_adamw*)rule)->grad_type = kind;
     Py_BEGIN_ALLOW_THREADS
     rc = sasgd_applyAdamW((const sasgd_adamw*)rule, (const sasgd_tensor*)tensors, count, grads, (int32_t)c, stale, (const sasgd_moments*)moments, step,
-                          (const int64_t*)step_dev, (const float*)factor, stream, err, sizeof(err));
+                          (const int64_t*)step_dev, (const float*)factor.data, stream, err, sizeof(err));
     Py_END_ALLOW_THREADS
   }
   PyMem_Free(grads);
-  if (bad) return NULL;
+  if (failed) return NULL;
   if (rc) return raise_code(rc, err);
+  Py_RETURN_NONE;
+}
+
+/* A tensor [images, ..., channels] as images of evenly spaced pixels with their channels side by side. */
+static int pixels(const char* name, const view* v, int64_t* positions, int64_t* image, int64_t* pixel) {
+  int k;
+  const int last = v->dims - 1;
+  *positions = 1;
+  if (v->dims < 2) return bad(PyExc_ValueError, name, "must be [images, ..., channels]");
+  *pixel = v->shape[last];
+  if (v->shape[last] > 1 && v->stride[last] != 1) return bad(PyExc_ValueError, name, "must have its channels last, side by side");
+  for (k = last - 1; k >= 1; k--) {
+    if (v->shape[k] == 1) continue;
+    if (*positions == 1) *pixel = v->stride[k];
+    else if (v->stride[k] != *pixel * *positions) return bad(PyExc_ValueError, name, "must have its positions evenly apart");
+    *positions *= v->shape[k];
+  }
+  *image = v->shape[0] > 1 ? v->stride[0] : *pixel * *positions;
+  return 0;
+}
+static int same_shape(const view* a, const view* b) {
+  return a->dims == b->dims && a->kind == b->kind && memcmp(a->shape, b->shape, sizeof(int64_t) * (size_t)a->dims) == 0;
+}
+
+/* x, y (or dy; may be None), scale and shift (None: none) of a group normalisation, checked, and its shape. */
+static int norm_shape(PyObject* ox, PyObject* oy, PyObject* oscale, PyObject* oshift, int32_t groups, int32_t activation, double eps, int device, view* x, view* y,
+                      void** scale, void** shift, sasgd_norm_shape* s) {
+  int64_t p;
+  view v;
+  int k, type = KIND_OTHER;
+  PyObject* params[2] = {oscale, oshift};
+  void** data[2] = {scale, shift};
+  memset(s, 0, sizeof(*s));
+  if (view_of(ox, x)) return -1;
+  if (x->kind == KIND_OTHER) return bad(PyExc_TypeError, "x", "must be float32 or bfloat16");
+  if (device >= 0 && x->device != device) return bad(PyExc_ValueError, "x", "is not on the current device");
+  if (pixels("x", x, &s->positions, &s->x_image, &s->x_pixel)) return -1;
+  if (oy != Py_None) {
+    if (view_of(oy, y)) return -1;
+    if (!same_shape(x, y)) return bad(PyExc_ValueError, "y", "must have the shape and the type of x");
+    if (y->device != device) return bad(PyExc_ValueError, "y", "is not on the current device");
+    if (pixels("y", y, &p, &s->y_image, &s->y_pixel)) return -1;
+  }
+  s->images = x->shape[0];
+  s->channels = x->shape[x->dims - 1] > INT32_MAX ? INT32_MAX : (int32_t)x->shape[x->dims - 1];
+  for (k = 0; k < 2; k++) {
+    *data[k] = NULL;
+    if (params[k] == Py_None) continue;
+    if (want(params[k], "a parameter", device, KIND_OTHER, 0, &v)) return -1;
+    if (elements(&v) != s->channels) return bad(PyExc_ValueError, "a parameter", "must have one value per channel");
+    if (v.kind == KIND_OTHER || (type != KIND_OTHER && v.kind != type)) return bad(PyExc_TypeError, "scale and shift", "must both be float32 or both bfloat16");
+    type = v.kind;
+    *data[k] = v.data;
+  }
+  s->groups = groups;
+  s->type = x->kind;
+  s->param_type = type == KIND_OTHER ? SASGD_FP32 : type;
+  s->activation = activation;
+  s->eps = (float)eps;
+  return 0;
+}
+
+/* group_norm_workspace(x, groups, gradient) */
+static PyObject* group_norm_workspace(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  sasgd_norm_shape s;
+  int32_t groups, gradient;
+  void *scale, *shift;
+  size_t bytes;
+  view x, y;
+  NARGS(3);
+  if (integer32(a[1], &groups) || integer32(a[2], &gradient) || norm_shape(a[0], Py_None, Py_None, Py_None, groups, 0, 1.0, -1, &x, &y, &scale, &shift, &s)) return NULL;
+  if (sasgd_groupNormWorkspace(&s, gradient, &bytes)) return raise_code(SASGD_EINVAL, "groupNormWorkspace: bad shape");
+  return PyLong_FromSize_t(bytes);
+}
+
+/* group_norm(x, scale, shift, groups, y, stats, activation, eps, workspace, device, stream) */
+static PyObject* group_norm(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  sasgd_norm_shape s;
+  int32_t groups, activation, device;
+  void *scale, *shift, *work, *stream;
+  size_t bytes;
+  double eps;
+  view x, y, stats;
+  char err[256] = "";
+  int rc;
+  NARGS(11);
+  eps = PyFloat_AsDouble(a[7]);
+  if (PyErr_Occurred()) return NULL;
+  if (integer32(a[3], &groups) || integer32(a[6], &activation) || integer32(a[9], &device) || address(a[10], &stream)) return NULL;
+  if (a[4] == Py_None) {
+    PyErr_SetString(PyExc_TypeError, "y must be a tensor");
+    return NULL;
+  }
+  if (norm_shape(a[0], a[4], a[1], a[2], groups, activation, eps, device, &x, &y, &scale, &shift, &s) || workspace_of(a[8], device, &work, &bytes)) return NULL;
+  stats.data = NULL;
+  if (a[5] != Py_None && want(a[5], "stats", device, SASGD_FP32, 2 * s.images * groups, &stats)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = sasgd_groupNorm(&s, x.data, scale, shift, y.data, (float*)stats.data, work, bytes, stream, err, sizeof(err));
+  Py_END_ALLOW_THREADS
+  if (rc) return raise_code(rc, err);
+  Py_RETURN_NONE;
+}
+
+/* group_norm_gradient(x, scale, shift, groups, stats, dy, dx, dscale, dshift, activation, workspace, device, stream) */
+static PyObject* group_norm_gradient(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  sasgd_norm_shape s;
+  int32_t groups, activation, device;
+  int64_t p, image, pixel;
+  void *scale, *shift, *work, *stream;
+  size_t bytes;
+  view x, dy, stats, dx, dscale, dshift;
+  char err[256] = "";
+  int rc;
+  NARGS(13);
+  if (integer32(a[3], &groups) || integer32(a[9], &activation) || integer32(a[11], &device) || address(a[12], &stream)) return NULL;
+  if (a[5] == Py_None) {
+    PyErr_SetString(PyExc_TypeError, "dy must be a tensor");
+    return NULL;
+  }
+  if (norm_shape(a[0], a[5], a[1], a[2], groups, activation, 1.0, device, &x, &dy, &scale, &shift, &s) || workspace_of(a[10], device, &work, &bytes) ||
+      want(a[4], "stats", device, SASGD_FP32, 2 * s.images * groups, &stats))
+    return NULL;
+  dx.data = dscale.data = dshift.data = NULL;
+  if (a[6] != Py_None) {
+    if (view_of(a[6], &dx) || pixels("dx", &dx, &p, &image, &pixel)) return NULL;
+    if (dx.device != device || !same_shape(&x, &dx) || image != s.y_image || pixel != s.y_pixel) {
+      PyErr_SetString(PyExc_ValueError, "dx must have the shape, type and device of x and the strides of dy");
+      return NULL;
+    }
+  }
+  if ((a[7] != Py_None && want(a[7], "dscale", device, SASGD_FP32, s.channels, &dscale)) || (a[8] != Py_None && want(a[8], "dshift", device, SASGD_FP32, s.channels, &dshift)))
+    return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = sasgd_groupNormGradient(&s, x.data, scale, shift, (const float*)stats.data, dy.data, dx.data, (float*)dscale.data, (float*)dshift.data, work, bytes, stream, err,
+                               sizeof(err));
+  Py_END_ALLOW_THREADS
+  if (rc) return raise_code(rc, err);
+  Py_RETURN_NONE;
+}
+
+/* set_tensor_class(torch.Tensor, torch.float32, torch.bfloat16) */
+static PyObject* set_tensor_class(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  PyObject* capsule;
+  NARGS(3);
+  Py_INCREF(a[0]);
+  Py_INCREF(a[1]);
+  Py_INCREF(a[2]);
+  tensor_class = a[0];
+  fp32_type = a[1];
+  bf16_type = a[2];
+  capsule = PyObject_GetAttrString(a[0], "__dlpack_c_exchange_api__");
+  if (capsule) {
+    const DLPackExchangeAPI* api = (const DLPackExchangeAPI*)PyCapsule_GetPointer(capsule, "dlpack_exchange_api");
+    if (api && api->header.version.major == DLPACK_MAJOR_VERSION && api->dltensor_from_py_object_no_sync) exchange = api;
+    Py_DECREF(capsule);
+  }
+  PyErr_Clear();
   Py_RETURN_NONE;
 }
 
@@ -427,6 +679,10 @@ static PyMethodDef methods[] = {FAST(get_minibatch),
                                 FAST(apply_update_no_alloc),
                                 FAST(gradient_norm),
                                 FAST(apply_adamw),
+                                FAST(group_norm_workspace),
+                                FAST(group_norm),
+                                FAST(group_norm_gradient),
+                                FAST(set_tensor_class),
                                 {"sum_gradients", sum_gradients, METH_O, NULL},
                                 {"apply_update", apply_update, METH_O, NULL},
                                 {"timestamp", timestamp, METH_O, NULL},
@@ -440,10 +696,11 @@ PyMODINIT_FUNC PyInit__fastcalls(void) {
   s_ctypes = PyUnicode_InternFromString("ctypes");
   s_data = PyUnicode_InternFromString("data");
   s_dtype = PyUnicode_InternFromString("dtype");
-  s_numel = PyUnicode_InternFromString("numel");
-  s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+  s_shape = PyUnicode_InternFromString("shape");
+  s_stride = PyUnicode_InternFromString("stride");
+  s_element_size = PyUnicode_InternFromString("element_size");
   s_get_device = PyUnicode_InternFromString("get_device");
-  if (!s_data_ptr || !s_ctypes || !s_data || !s_dtype || !s_numel || !s_is_contiguous || !s_get_device) return NULL;
+  if (!s_data_ptr || !s_ctypes || !s_data || !s_dtype || !s_shape || !s_stride || !s_element_size || !s_get_device) return NULL;
   Py_INCREF(PyExc_RuntimeError);
   error_class = PyExc_RuntimeError;
   return PyModule_Create(&module);
