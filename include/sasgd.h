@@ -254,8 +254,8 @@ int sasgd_momentElements(const int64_t* numel, int32_t count, int64_t* out_eleme
  *     m <- beta1 m + (1 - beta1) g;   v <- beta2 v + (1 - beta2) g^2
  *     theta_out = theta_in (1 - rate weight_decay) - rate / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + epsilon)
  * rate g is the sum of coef_l g_l that sumGradients defines; the step's length follows the staleness although the moments take
- * the gradients' size out of it.  With c = 1 and staleness 0 this is AdamW at the rate alpha0.  All arithmetic is fp32, each operation
- * rounded by itself.
+ * the gradients' size out of it.  With c = 1 and staleness 0 this is AdamW at the rate alpha0.  All arithmetic is fp32; what is kept in the
+ * moments is rounded operation by operation, the weight's move takes a root and a reciprocal of 1 ulp.
  *   grads_dev: HOST array of count c device pointers, those of tensor k at [k c .. k c + c); staleness: HOST int32 [c];
  *   step: t >= 1; step_dev: optional device int64 that holds t instead (a captured graph reads it at every replay);
  *   factor_dev: optional device float, gradientNorm's out_dev + 1; where it holds NaN the step is left out: the moments stay, and

@@ -30,7 +30,7 @@ int refuse(char* err, size_t err_len, int code, const char* fmt, ...) {
   } while (0)
 
 inline int64_t blocks_of(int64_t numel) { return (numel + kMomentBlock - 1) / kMomentBlock; }
-constexpr int64_t kMostElements = (int64_t)1 << 35;     // of a tensor and of a call: its launch stays below 2^32 lanes
+constexpr int64_t kMostElements = (int64_t)1 << 34;     // of a tensor and of a call: its launch stays below 2^32 lanes
 
 // ---------------------------------------------------------------- group normalisation
 constexpr int kWideChannels = 4096, kNarrowChannels = 1024;   // sums by channel of a workgroup lie in LDS
@@ -169,7 +169,7 @@ int sasgd_gradientNorm(const void* const* grads_dev, const int64_t* numel, int32
     if (numel[k] > 0 && (!grads_dev[k] || ((uintptr_t)grads_dev[k] & (bf ? 1 : 3)))) REFUSE("gradientNorm: tensor %d is null or not aligned to its elements", (int)k);
     blocks += blocks_of(numel[k]);
   }
-  if (blocks * kMomentBlock > kMostElements) REFUSE("gradientNorm: more than 2^35 elements");
+  if (blocks * kMomentBlock > kMostElements) REFUSE("gradientNorm: more than 2^34 elements");
   static_assert(kNormPartials * sizeof(double) <= SASGD_NORM_WORKSPACE, "partial sums do not fit the workspace");
   NormLaunch a;
   memset(&a, 0, sizeof(a));
@@ -191,10 +191,10 @@ int sasgd_gradientNorm(const void* const* grads_dev, const int64_t* numel, int32
       tab.first[tab.n + 1] = tab.first[tab.n] + (uint32_t)blocks_of(numel[k]);
       tab.n++;
     }
-    TRY_HIP(launch_norm_partials(a, bf, (hipStream_t)stream), "gradientNorm");
+    a.last = k == count;
+    TRY_HIP(launch_norm(a, bf, (hipStream_t)stream), "gradientNorm");
     a.add = 1;
   } while (k < count);
-  TRY_HIP(launch_norm_finish(a, (hipStream_t)stream), "gradientNorm");
   return SASGD_OK;
 }
 
@@ -239,7 +239,7 @@ int sasgd_applyAdamW(const sasgd_adamw* rule, const sasgd_tensor* tensors, int32
     has_shadow = has_shadow || t.shadow_out;
     blocks += blocks_of(t.numel);
   }
-  if (blocks * kMomentBlock > kMostElements) REFUSE("applyAdamW: more than 2^35 elements");
+  if (blocks * kMomentBlock > kMostElements) REFUSE("applyAdamW: more than 2^34 elements");
   if (blocks == 0) return SASGD_OK;
   if (!moments->m || !moments->v || (((uintptr_t)moments->m | (uintptr_t)moments->v) & 15)) REFUSE("applyAdamW: moments must be 16-byte aligned device pointers");
   if (e4m3 && (!moments->m_scale || !moments->v_scale || (((uintptr_t)moments->m_scale | (uintptr_t)moments->v_scale) & 3)))
@@ -264,7 +264,7 @@ int sasgd_applyAdamW(const sasgd_adamw* rule, const sasgd_tensor* tensors, int32
   a.log_beta2 = log(rule->beta2);
   if (!step_dev) {
     a.pace = (float)(a.rate / -expm1((double)step * a.log_beta1));
-    a.vcorr = (float)(1.0 / -expm1((double)step * a.log_beta2));
+    a.root = (float)sqrt(1.0 / -expm1((double)step * a.log_beta2));
   }
   a.beta1 = (float)rule->beta1;
   a.rest1 = (float)(1.0 - rule->beta1);

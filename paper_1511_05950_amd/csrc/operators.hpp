@@ -36,7 +36,7 @@ struct AdamwLaunch {
   const int64_t* step_dev;
   int64_t step;
   double rate, log_beta1, log_beta2;
-  float pace, vcorr;         // rate / (1 - beta1^step), 1 / (1 - beta2^step); computed from step_dev where there is one
+  float pace, root;          // rate / (1 - beta1^step), sqrt(1 / (1 - beta2^step)); computed from step_dev where there is one
   float beta1, rest1, beta2, rest2, epsilon, keep;   // rest = 1 - beta, keep = 1 - rate weight_decay
 };
 hipError_t launch_adamw(const AdamwLaunch& a, bool grad_bf16, bool e4m3, hipStream_t stream);
@@ -48,11 +48,11 @@ struct NormLaunch {
   float* out;                // norm, factor
   float max_norm;
   int32_t add;               // partial[] holds the sums of the launches before
-  int32_t grid;
+  int32_t last;              // no more tensors behind these: norm and factor follow
+  int32_t grid;              // workgroups, the same in all launches of a call (norm_grid)
 };
 int norm_grid(int64_t blocks);
-hipError_t launch_norm_partials(const NormLaunch& a, bool bf16, hipStream_t stream);
-hipError_t launch_norm_finish(const NormLaunch& a, hipStream_t stream);
+hipError_t launch_norm(const NormLaunch& a, bool bf16, hipStream_t stream);
 
 // ---------------------------------------------------------------- group normalisation (group_norm.hip)
 // How a call is cut into workgroups (group_norm_plan).
