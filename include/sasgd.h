@@ -24,7 +24,8 @@
  *
  * Flat parameter order (weights, gradients, momentum alike): layers in network order; for
  * each convolution the weights [Cout][Cin][kh][kw] then the bias [Cout]; for each fully
- * connected layer the weights [out][in] (in = C,H,W flattened in that order) then the bias.
+ * connected layer the weights [out][in] (in = C,H,W flattened in that order) then the bias; for each
+ * group normalisation the scales [C] then the shifts [C].
  */
 #ifndef SASGD_H
 #define SASGD_H
@@ -51,7 +52,7 @@ enum {
 enum { SASGD_NET_NONE = 0, SASGD_NET_CIFAR3 = 1, SASGD_NET_ALEX8 = 2, SASGD_NET_CUSTOM = 3 };
 enum { SASGD_FP32 = 0, SASGD_BF16 = 1 };
 enum { SASGD_LR_PER_GRADIENT = 0, SASGD_LR_MEAN_STALENESS = 1, SASGD_LR_CONSTANT = 2 };
-enum { SASGD_CONV = 0, SASGD_MAXPOOL = 1, SASGD_AVGPOOL = 2, SASGD_RELU = 3, SASGD_FC = 4 };
+enum { SASGD_CONV = 0, SASGD_MAXPOOL = 1, SASGD_AVGPOOL = 2, SASGD_RELU = 3, SASGD_FC = 4, SASGD_GROUPNORM = 5 };
 /* flags */
 enum { SASGD_FLAG_FLAT_FC_GRADIENT = 1, SASGD_FLAG_EAGER_UPDATES = 2 };   /* see sasgd_config.flags */
 
@@ -60,8 +61,10 @@ enum { SASGD_FLAG_FLAT_FC_GRADIENT = 1, SASGD_FLAG_EAGER_UPDATES = 2 };   /* see
  *   CONV:    units = output channels, window x window kernel, stride, pad (zero padding)
  *   MAXPOOL / AVGPOOL: window, stride; output size ceil((H - window)/stride) + 1, windows clipped
  *            at the border, the average taken over the in-bounds elements
- *   RELU:    must directly follow a CONV, FC or pooling layer
- *   FC:      units = outputs                                                              */
+ *   RELU:    must directly follow a CONV, FC, pooling or GROUPNORM layer
+ *   FC:      units = outputs
+ *   GROUPNORM: units = groups; group normalisation (see sasgd_groupNorm) with eps 1e-5, a scale and a shift per channel; at most
+ *            4 096 channels, 1 024 where their number is no multiple of 8 (FP32 compute: of 4).  Behind an FC layer: over groups of its outputs. */
 typedef struct {
   int32_t kind, units, window, stride, pad;
 } sasgd_layer;
@@ -264,6 +267,14 @@ int sasgd_momentElements(const int64_t* numel, int32_t count, int64_t* out_eleme
 int sasgd_applyAdamW(const sasgd_adamw* rule, const sasgd_tensor* tensors, int32_t count, const void* const* grads_dev, int32_t c,
                      const int32_t* staleness, const sasgd_moments* moments, int64_t step, const int64_t* step_dev,
                      const float* factor_dev, void* stream, char* err, size_t err_len);
+
+/* useAdamW: from the next applyUpdate on the context's server takes AdamW steps (applyAdamW, on the whole vector as one tensor) instead of the
+ * momentum rule; alpha0, lr_mode and weight_decay stay the context's, rule's beta1, beta2, epsilon, seed and kind of moments are read.  The
+ * moments, sasgd_momentElements of P, are the caller's, start as zeros and stay in use until the next useAdamW or the context's end;
+ * the steps count from 1 at the next update.  rule NULL: back to the momentum rule (its momentum is as it was).  Updates are enqueued
+ * before applyUpdate returns; gradients that learners hold as factors are written out first (SASGD_FLAG_FLAT_FC_GRADIENT saves that).
+ * copyMomentum fails with ESTATE meanwhile.  Errors: EINVAL (rule, moments), ESTATE while a window is closed. */
+int sasgd_useAdamW(sasgd_ctx* ctx, const sasgd_adamw* rule, const sasgd_moments* moments);
 
 /* ---- group normalisation ------------------------------------------------------------------ */
 

@@ -16,7 +16,7 @@ _SRC = os.path.join(_HERE, "cnn_oracle.c")
 _LIB = os.path.join(_HERE, "libcnn_oracle.so")
 _lib = None
 
-_TYPES = {"conv": 0, "maxpool": 1, "avgpool": 2, "relu": 3, "fc": 4}
+_TYPES = {"conv": 0, "maxpool": 1, "avgpool": 2, "relu": 3, "fc": 4, "groupnorm": 5}
 
 
 def build(force=False):

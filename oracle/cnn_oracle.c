@@ -38,10 +38,10 @@
 #include <stdlib.h>
 #include <string.h>
 
-enum { L_CONV = 0, L_MAXPOOL = 1, L_AVGPOOL = 2, L_RELU = 3, L_FC = 4 };
+enum { L_CONV = 0, L_MAXPOOL = 1, L_AVGPOOL = 2, L_RELU = 3, L_FC = 4, L_GROUPNORM = 5 };
 
 /* One row of the layer table passed in from Python: type, a, b, c, d
- *   conv: a=cout b=k c=stride d=pad;  pool: a=k b=stride;  fc: a=out            */
+ *   conv: a=cout b=k c=stride d=pad;  pool: a=k b=stride;  fc: a=out;  groupnorm: a=groups */
 typedef struct { int type, a, b, c, d; } olayer;
 
 static int pool_out(int n, int k, int s) {
@@ -260,6 +260,56 @@ void fc_backward(const double* x, const double* w, const double* dy, double* dx,
     }
 }
 
+/* ------------------------------------------------------------------ group normalisation */
+/* per image and group of C / G channels: z = (x - mean) / sqrt(var + 1e-5) * scale[c] + shift[c] */
+void groupnorm_forward(const double* x, const double* scale, const double* shift, double* y, int N, int C, int HW, int G) {
+  int per = C / G;
+#pragma omp parallel for collapse(2) schedule(static)
+  for (int n = 0; n < N; n++)
+    for (int g = 0; g < G; g++) {
+      size_t first = ((size_t)n * C + (size_t)g * per) * HW, count = (size_t)per * HW;
+      double mean = 0.0, var = 0.0;
+      for (size_t i = 0; i < count; i++) mean += x[first + i];
+      mean /= count;
+      for (size_t i = 0; i < count; i++) var += (x[first + i] - mean) * (x[first + i] - mean);
+      var /= count;
+      for (size_t i = 0; i < count; i++) {
+        int c = g * per + (int)(i / HW);
+        y[first + i] = (x[first + i] - mean) / sqrt(var + 1e-5) * scale[c] + shift[c];
+      }
+    }
+}
+
+/* the chain rule through mean and variance; dx may be NULL, dscale and dshift are overwritten */
+void groupnorm_backward(const double* x, const double* scale, const double* dy, double* dx, double* dscale, double* dshift, int N, int C, int HW, int G) {
+  int per = C / G;
+  for (int c = 0; c < C; c++) dscale[c] = dshift[c] = 0.0;
+#pragma omp parallel for schedule(static)
+  for (int g = 0; g < G; g++)
+    for (int n = 0; n < N; n++) {
+      size_t first = ((size_t)n * C + (size_t)g * per) * HW, count = (size_t)per * HW;
+      double mean = 0.0, var = 0.0, dvar = 0.0, dmean = 0.0;
+      for (size_t i = 0; i < count; i++) mean += x[first + i];
+      mean /= count;
+      for (size_t i = 0; i < count; i++) var += (x[first + i] - mean) * (x[first + i] - mean);
+      var /= count;
+      double dev = sqrt(var + 1e-5);
+      for (size_t i = 0; i < count; i++) {
+        int c = g * per + (int)(i / HW);
+        double d = x[first + i] - mean, dh = dy[first + i] * scale[c];
+        dscale[c] += dy[first + i] * d / dev;
+        dshift[c] += dy[first + i];
+        dvar += dh * d * -0.5 / (dev * dev * dev);
+        dmean += -dh / dev;
+      }
+      if (!dx) continue;
+      for (size_t i = 0; i < count; i++) {
+        int c = g * per + (int)(i / HW);
+        dx[first + i] = dy[first + i] * scale[c] / dev + dvar * 2.0 * (x[first + i] - mean) / count + dmean / count;
+      }
+    }
+}
+
 /* loss = (1/N) sum_n -log softmax(z_n)[y_n];   dz = (softmax(z) - onehot) / N */
 double softmax_ce(const double* z, const int* label, double* dz, int N, int K) {
   double loss = 0.0;
@@ -329,6 +379,10 @@ static double loss_gradient_scores(const olayer* layers, int nlayers, int C, int
           fc_forward(act[li], theta + pos, theta + pos + nw, act[li + 1], N, c * h * w, oc);
         pos += nw + oc;
       } break;
+      case L_GROUPNORM:
+        if (pos + 2 * c <= P) groupnorm_forward(act[li], theta + pos, theta + pos + c, act[li + 1], N, c, h * w, L->a);
+        pos += 2 * c;
+        break;
     }
     if (li + 1 < nlayers) round_array(act[li + 1], no, round_bf16);   /* the class scores stay unrounded */
     sc[3 * (li + 1)] = oc; sc[3 * (li + 1) + 1] = oh; sc[3 * (li + 1) + 2] = ow;
@@ -359,6 +413,7 @@ static double loss_gradient_scores(const olayer* layers, int nlayers, int C, int
           long nw = (long)oc * c * h * w;
           fc_backward(act[li], theta + off[li], d, dprev, grad + off[li], grad + off[li] + nw, N, c * h * w, oc);
         } break;
+        case L_GROUPNORM: groupnorm_backward(act[li], theta + off[li], d, dprev, grad + off[li], grad + off[li] + c, N, c, h * w, L->a); break;
       }
       free(d);
       d = dprev;
@@ -397,7 +452,8 @@ double cnn_class_scores(const olayer* layers, int nlayers, int C, int H, int W, 
  * term.  The tests ask for this number and take only cases in which every ReLU input is decided.
  * Exact mode only.  Returns min over all ReLU inputs with a non-zero term sum of |v| / (|b| + sum_k |w_k x_k|), where
  * the sum is that of the convolution or fully connected layer in front of the ReLU (a max pool in between passes the
- * winner's sum on, an average pool the average of its window's sums); 1.0 if the network has no ReLU; NaN when P does
+ * winner's sum on, an average pool the average of its window's sums, a group normalisation |scale| / deviation times the sum and
+ * its group's average one, plus |shift|); 1.0 if the network has no ReLU; NaN when P does
  * not match.
  */
 double cnn_min_relu_margin(const olayer* layers, int nlayers, int C, int H, int W, int N,
@@ -443,6 +499,25 @@ double cnn_min_relu_margin(const olayer* layers, int nlayers, int C, int H, int 
     } else if (L->type == L_AVGPOOL) {
       avgpool_forward(act, out, N * c, h, w, L->a, L->b);
       avgpool_forward(mag, mout, N * c, h, w, L->a, L->b);
+    } else if (L->type == L_GROUPNORM) {
+      int per = c / L->a;
+      const double *scale = theta + pos, *shift = theta + pos + c;
+      pos += 2 * c;
+      if (pos > P) { free(out); free(mout); free(act); free(mag); return NAN; }
+      groupnorm_forward(act, scale, shift, out, N, c, h * w, L->a);
+      for (int n = 0; n < N; n++)
+        for (int g = 0; g < L->a; g++) {
+          size_t first = ((size_t)n * c + (size_t)g * per) * h * w, count = (size_t)per * h * w;
+          double mean = 0.0, var = 0.0, size = 0.0;
+          for (size_t i = 0; i < count; i++) { mean += act[first + i]; size += mag[first + i]; }
+          mean /= count;
+          size /= count;
+          for (size_t i = 0; i < count; i++) var += (act[first + i] - mean) * (act[first + i] - mean);
+          for (size_t i = 0; i < count; i++) {
+            int ch = g * per + (int)(i / ((size_t)h * w));
+            mout[first + i] = fabs(scale[ch]) / sqrt(var / count + 1e-5) * (mag[first + i] + size) + fabs(shift[ch]);
+          }
+        }
     } else {   /* L_RELU */
       for (size_t i = 0; i < ni; i++) {
         if (mag[i] > 0.0) { double m = fabs(act[i]) / mag[i]; if (m < worst) worst = m; }
@@ -467,6 +542,7 @@ long cnn_num_params(const olayer* layers, int nlayers, int C, int H, int W) {
     if (L->type == L_CONV) { pos += (long)L->a * c * L->b * L->b + L->a; h = (h + 2 * L->d - L->b) / L->c + 1; w = (w + 2 * L->d - L->b) / L->c + 1; c = L->a; }
     else if (L->type == L_MAXPOOL || L->type == L_AVGPOOL) { h = pool_out(h, L->a, L->b); w = pool_out(w, L->a, L->b); }
     else if (L->type == L_FC) { pos += (long)L->a * c * h * w + L->a; c = L->a; h = 1; w = 1; }
+    else if (L->type == L_GROUPNORM) pos += 2 * c;
   }
   return pos;
 }

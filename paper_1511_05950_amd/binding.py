@@ -18,7 +18,7 @@ OK, EINVAL, ESTATE, ENOTREADY, ERANGE, EHIP, ENOMEM = 0, -1, -2, -3, -4, -5, -6
 NET_NONE, NET_CIFAR3, NET_ALEX8, NET_CUSTOM = 0, 1, 2, 3
 FP32, BF16 = 0, 1
 LR_PER_GRADIENT, LR_MEAN_STALENESS, LR_CONSTANT = 0, 1, 2
-LAYER_KINDS = {"conv": 0, "maxpool": 1, "avgpool": 2, "relu": 3, "fc": 4}
+LAYER_KINDS = {"conv": 0, "maxpool": 1, "avgpool": 2, "relu": 3, "fc": 4, "groupnorm": 5}
 LR_MODES = {"per_gradient": 0, "mean_staleness": 1, "constant": 2}
 FLAG_FLAT_FC_GRADIENT = 1
 FLAG_EAGER_UPDATES = 2
@@ -34,7 +34,7 @@ EXPORTS = [
     "sasgd_copyWeights", "sasgd_copyGradient", "sasgd_copyMomentum", "sasgd_gradientPtr",
     "sasgd_setProfiling", "sasgd_phaseTime", "sasgd_last_error", "sasgd_version",
     "sasgd_evaluate", "sasgd_setBaseRate", "sasgd_setPixelMean", "sasgd_factoredParams",
-    "sasgd_applyUpdateNoAlloc", "sasgd_flush", "sasgd_gradientNorm", "sasgd_momentElements", "sasgd_applyAdamW",
+    "sasgd_applyUpdateNoAlloc", "sasgd_flush", "sasgd_gradientNorm", "sasgd_momentElements", "sasgd_applyAdamW", "sasgd_useAdamW",
     "sasgd_groupNorm", "sasgd_groupNormGradient", "sasgd_groupNormWorkspace",
 ]
 
@@ -135,6 +135,7 @@ def load():
         lib.sasgd_momentElements.argtypes = [P(i64), i32, P(i64)]
         lib.sasgd_applyAdamW.argtypes = [P(SasgdAdamw), P(SasgdTensor), i32, P(vp), i32, P(i32), P(SasgdMoments), i64, vp, vp, vp, ctypes.c_char_p,
                                          ctypes.c_size_t]
+        lib.sasgd_useAdamW.argtypes = [vp, P(SasgdAdamw), P(SasgdMoments)]
         lib.sasgd_last_error.argtypes = [vp]
         lib.sasgd_last_error.restype = ctypes.c_char_p
         lib.sasgd_version.restype = ctypes.c_char_p
@@ -192,7 +193,7 @@ class Sasgd:
                     arr[k].units, arr[k].window, arr[k].stride, arr[k].pad = vals[:4]
                 elif L[0] in ("maxpool", "avgpool"):
                     arr[k].window, arr[k].stride = vals[:2]
-                elif L[0] == "fc":
+                elif L[0] in ("fc", "groupnorm"):
                     arr[k].units = vals[0]
             self._layers = arr
             cfg.layers = arr
@@ -263,6 +264,18 @@ class Sasgd:
 
     def applyUpdate(self):
         return _fast.apply_update(self._h.value)
+
+    def useAdamW(self, m, v, m_scale=None, v_scale=None, beta1=0.9, beta2=0.999, eps=1e-8, seed=0):
+        """From the next update on the server takes AdamW steps (m None: the momentum rule again).  Moments as for AdamW, of a
+        vector of P weights; alpha0, lr_mode and weight_decay stay the context's."""
+        if m is None:
+            self._check(load().sasgd_useAdamW(self._h, None, None))
+            self._keep_moments = None
+            return
+        moments, small = _moments(m, v, m_scale, v_scale, (self.P + 255) // 256 * 256)
+        rule = SasgdAdamw(0, MOMENTS_E4M3 if small else MOMENTS_FP32, FP32, seed & 0xFFFFFFFF, 0.0, beta1, beta2, eps, 0.0)
+        self._check(load().sasgd_useAdamW(self._h, ctypes.byref(rule), ctypes.byref(moments)))
+        self._keep_moments = (m, v, m_scale, v_scale)
 
     def flush(self):
         self._check(load().sasgd_flush(self._h))
@@ -392,6 +405,19 @@ def gradientNorm(grads, out, max_norm=0.0, workspace=None, stream=None):
     _fast.gradient_norm(grads, max_norm, out, workspace, device, stream)
 
 
+def _moments(m, v, m_scale, v_scale, elements):
+    """(the C structure, whether they are 8 bits wide), checked."""
+    _want("m", m, ("float32", "float8_e4m3fn"), elements)
+    _want("v", v, (str(m.dtype)[6:],), elements)
+    small = m.element_size() == 1
+    if small:
+        if m_scale is None or v_scale is None:
+            raise ValueError("8-bit moments need their scales")
+        _want("m_scale", m_scale, ("float32",), elements // 256)
+        _want("v_scale", v_scale, ("float32",), elements // 256)
+    return SasgdMoments(_addr(m), _addr(v), _addr(m_scale) if small else None, _addr(v_scale) if small else None), small
+
+
 def momentElements(weights):
     """How many elements each moment of these tensors has (sasgd_momentElements)."""
     numel = (ctypes.c_int64 * max(1, len(weights)))(*[t.numel() for t in weights])
@@ -427,15 +453,7 @@ class AdamW:
             if s is not None:
                 _want("copies", s, ("bfloat16",), w.numel())
             e.numel, e.theta_in, e.theta_out, e.shadow_out = w.numel(), _addr(w), _addr(o), _addr(s)
-        _want("m", m, ("float32", "float8_e4m3fn"), elements)
-        _want("v", v, (str(m.dtype)[6:],), elements)
-        small = m.element_size() == 1
-        if small:
-            if m_scale is None or v_scale is None:
-                raise ValueError("8-bit moments need their scales")
-            _want("m_scale", m_scale, ("float32",), elements // 256)
-            _want("v_scale", v_scale, ("float32",), elements // 256)
-        self._moments = SasgdMoments(_addr(m), _addr(v), _addr(m_scale) if small else None, _addr(v_scale) if small else None)
+        self._moments, small = _moments(m, v, m_scale, v_scale, elements)
         self._rule = SasgdAdamw(LR_MODES[lr_mode] if isinstance(lr_mode, str) else lr_mode, MOMENTS_E4M3 if small else MOMENTS_FP32, FP32,
                                 seed & 0xFFFFFFFF, alpha0, beta1, beta2, eps, weight_decay)
         self._keep = (weights, outs, copies, m, v, m_scale, v_scale)

@@ -248,6 +248,47 @@ hipError_t enqueue_updates(sasgd_ctx* ctx, int n) {
   return e;
 }
 
+// One update by AdamW: the window's gradients, those held as factors written out first, and the repacked filters of the new version.
+int enqueue_adamw(sasgd_ctx* ctx) {
+  const int64_t i = ctx->timestamp;
+  const bool bf = ctx->cfg.compute == SASGD_BF16;
+  const size_t Ppad = ((size_t)ctx->P + 63) & ~(size_t)63;
+  const void* grads[kMaxLearners];
+  int32_t taus[kMaxLearners];
+  hipError_t e = hipSuccess;
+  prof_begin(ctx, 1);
+  for (int l = 0; l < ctx->window_count && e == hipSuccess; l++) {
+    const Pending& p = ctx->pending[(size_t)l];
+    if (p.factors_ws) e = expand_factored(ctx, ctx->learners[(size_t)p.learner]);
+    grads[l] = p.grad;
+    taus[l] = p.staleness;
+  }
+  if (e != hipSuccess) {
+    prof_end(ctx);
+    return fail_hip(ctx, e, "applyUpdate");
+  }
+  bf16_t* slot = bf ? ctx->ring_b16 + (size_t)slot_of(ctx, i + 1) * ctx->slot_elems_b16 : nullptr;
+  sasgd_tensor t;
+  t.numel = ctx->P;
+  t.theta_in = bf ? ctx->ring_f32 : ctx->ring_f32 + (size_t)slot_of(ctx, i) * ctx->slot_elems_f32;
+  t.theta_out = bf ? ctx->ring_f32 : ctx->ring_f32 + (size_t)slot_of(ctx, i + 1) * ctx->slot_elems_f32;
+  t.shadow_out = slot;
+  sasgd_adamw rule = ctx->adamw_rule;
+  rule.lr_mode = ctx->cfg.lr_mode;
+  rule.grad_type = SASGD_FP32;
+  rule.alpha0 = ctx->cfg.alpha0;
+  rule.weight_decay = ctx->cfg.weight_decay;
+  char err[256] = "";
+  const int rc = sasgd_applyAdamW(&rule, &t, 1, grads, ctx->window_count, taus, &ctx->adamw_moments, i - ctx->adamw_from + 1, nullptr, nullptr, ctx->stream, err, sizeof(err));
+  prof_end(ctx);
+  if (rc != SASGD_OK) return fail(ctx, rc, std::string("applyUpdate: ") + err);
+  if (bf && ctx->net) {
+    e = net_prepare_version(ctx->net, slot, slot + Ppad, ctx->stream);
+    if (e != hipSuccess) return fail_hip(ctx, e, "applyUpdate");
+  }
+  return SASGD_OK;
+}
+
 // Launches the kernels of every deferred update, in order, as few passes over the vector as the tables allow.
 int flush_updates(sasgd_ctx* ctx) {
   while (!ctx->deferred.empty()) {
@@ -265,6 +306,20 @@ int flush_updates(sasgd_ctx* ctx) {
     ctx->deferred.erase(ctx->deferred.begin(), ctx->deferred.begin() + n);
     if (e != hipSuccess) return fail_hip(ctx, e, "applyUpdate");
   }
+  return SASGD_OK;
+}
+
+// The window's gradients have been taken: learners and server move on to the next timestamp.
+int close_update(sasgd_ctx* ctx, int64_t* out_new_timestamp) {
+  for (int l = 0; l < ctx->window_count; l++) {
+    const int lr = ctx->pending[(size_t)l].learner;
+    if (lr >= 0) ctx->learners[(size_t)lr].grad_state = GRAD_NONE;
+  }
+  ctx->pending.erase(ctx->pending.begin(), ctx->pending.begin() + ctx->window_count);
+  ctx->window_closed = false;
+  ctx->window_count = 0;
+  ctx->timestamp += 1;      // every weight update increments the timestamp by one (Section 2.1)
+  if (out_new_timestamp) *out_new_timestamp = ctx->timestamp;
   return SASGD_OK;
 }
 
@@ -582,6 +637,11 @@ int sasgd_applyUpdate(sasgd_ctx* ctx, int64_t* out_new_timestamp) {
       if (L.has_weights && !L.evaluated && L.pulled_version == evicted)
         return fail(ctx, SASGD_ERANGE, "applyUpdate: a learner still holds the version this update would overwrite");
   }
+  if (ctx->adamw) {                      // (no update is deferred under this rule)
+    const int rc = enqueue_adamw(ctx);
+    if (rc != SASGD_OK) return rc;
+    return close_update(ctx, out_new_timestamp);
+  }
   DeferredUpdate d;
   d.i = i;
   float abar = 0.f;
@@ -603,21 +663,44 @@ int sasgd_applyUpdate(sasgd_ctx* ctx, int64_t* out_new_timestamp) {
     const int rc = flush_updates(ctx);
     if (rc != SASGD_OK) return rc;
   }
-  const int c_now = ctx->window_count;
   ctx->deferred.push_back(std::move(d));
   if (!defer) {
     const int rc = flush_updates(ctx);
     if (rc != SASGD_OK) { ctx->deferred.clear(); return rc; }
   }
-  for (int l = 0; l < c_now; l++) {
-    const int lr = ctx->pending[(size_t)l].learner;
-    if (lr >= 0) ctx->learners[(size_t)lr].grad_state = GRAD_NONE;
+  return close_update(ctx, out_new_timestamp);
+}
+
+int sasgd_useAdamW(sasgd_ctx* ctx, const sasgd_adamw* rule, const sasgd_moments* moments) {
+  if (!ctx) return SASGD_EINVAL;
+  if (ctx->window_closed) return fail(ctx, SASGD_ESTATE, "useAdamW: a window is closed; call applyUpdate first");
+  {
+    const int rc = flush_updates(ctx);
+    if (rc != SASGD_OK) return rc;
   }
-  ctx->pending.erase(ctx->pending.begin(), ctx->pending.begin() + c_now);
-  ctx->window_closed = false;
-  ctx->window_count = 0;
-  ctx->timestamp = i + 1;   // every weight update increments the timestamp by one (Section 2.1)
-  if (out_new_timestamp) *out_new_timestamp = ctx->timestamp;
+  if (!rule) {
+    ctx->adamw = false;
+    return SASGD_OK;
+  }
+  if (!moments) return fail(ctx, SASGD_EINVAL, "useAdamW: null moments");
+  // the checks of a step on an empty list of tensors, and of the moments it will need
+  sasgd_adamw r = *rule;
+  r.lr_mode = ctx->cfg.lr_mode;
+  r.grad_type = SASGD_FP32;
+  r.alpha0 = ctx->cfg.alpha0;
+  r.weight_decay = ctx->cfg.weight_decay;
+  const int32_t tau = 0;
+  char err[256] = "";
+  const int rc = sasgd_applyAdamW(&r, nullptr, 0, nullptr, 1, &tau, moments, 1, nullptr, nullptr, ctx->stream, err, sizeof(err));
+  if (rc != SASGD_OK) return fail(ctx, rc, std::string("useAdamW: ") + err);
+  const bool e4m3 = r.moments == SASGD_MOMENTS_E4M3;
+  if (!moments->m || !moments->v || (((uintptr_t)moments->m | (uintptr_t)moments->v) & 15) ||
+      (e4m3 && (!moments->m_scale || !moments->v_scale || (((uintptr_t)moments->m_scale | (uintptr_t)moments->v_scale) & 3))))
+    return fail(ctx, SASGD_EINVAL, "useAdamW: moments must be 16-byte aligned device pointers, e4m3 ones with scales");
+  ctx->adamw = true;
+  ctx->adamw_rule = r;
+  ctx->adamw_moments = *moments;
+  ctx->adamw_from = ctx->timestamp;
   return SASGD_OK;
 }
 
@@ -753,6 +836,7 @@ int sasgd_copyGradient(sasgd_ctx* ctx, int32_t learner, float* host_out) {
 
 int sasgd_copyMomentum(sasgd_ctx* ctx, float* host_out) {
   if (!ctx || !host_out) return SASGD_EINVAL;
+  if (ctx->adamw) return fail(ctx, SASGD_ESTATE, "copyMomentum: the server's rule is AdamW, whose moments are the caller's");
   {
     const int rc = flush_updates(ctx);
     if (rc != SASGD_OK) return rc;

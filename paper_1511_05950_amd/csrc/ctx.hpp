@@ -176,6 +176,10 @@ struct sasgd_ctx {
   size_t slot_elems_b16 = 0;         // elements per bf16 slot (P rounded up + packed filters)
   size_t slot_elems_f32 = 0;         // FP32 compute: elements per ring slot (P rounded up to 64)
   float* v = nullptr;                // momentum [P]
+  bool adamw = false;                // the server's rule is AdamW (sasgd_useAdamW), from timestamp adamw_from on
+  sasgd_adamw adamw_rule;
+  sasgd_moments adamw_moments;
+  int64_t adamw_from = 0;
   float* sum_buf = nullptr;          // [kSumStretch] partial result of windows that take two passes (two_pass_update), else nullptr
   std::vector<sasgd::Learner> learners;
   std::vector<sasgd::Pending> pending;

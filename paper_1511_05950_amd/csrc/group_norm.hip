@@ -862,10 +862,10 @@ GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient,
   return p;
 }
 
-size_t group_norm_part_bytes(const GroupNormShape& s, const GroupNormPlan& p) { return p.whole ? 0 : (size_t)s.images * p.chunks * s.groups * 8; }
-size_t group_norm_sum_bytes(const GroupNormShape& s, const GroupNormPlan& p) {
+size_t group_norm_sums_at(const GroupNormShape& s, const GroupNormPlan& p) { return p.whole ? 0 : ((size_t)s.images * p.chunks * s.groups * 8 + 15) / 16 * 16; }
+size_t group_norm_scratch_bytes(const GroupNormShape& s, const GroupNormPlan& p, bool gradient) {
   const int64_t rows = s.images * p.chunks;
-  return (size_t)(rows + finish_splits(rows)) * s.channels * 8;
+  return group_norm_sums_at(s, p) + (gradient ? (size_t)(rows + finish_splits(rows)) * s.channels * 8 : 0);
 }
 
 static uint32_t workgroups(const GroupNormArgs& a) {

@@ -10,10 +10,11 @@
 #include <vector>
 
 #include "kernels.hpp"
+#include "operators.hpp"
 
 namespace sasgd {
 
-enum OpKind { OP_CONV, OP_POOL_MAX, OP_POOL_AVG, OP_FLATTEN };
+enum OpKind { OP_CONV, OP_POOL_MAX, OP_POOL_AVG, OP_FLATTEN, OP_GROUPNORM };
 
 struct Op {
   OpKind kind;
@@ -21,10 +22,11 @@ struct Op {
   bool is_fc = false;
   bool out_f32 = false;        // output kept in fp32 (class scores)
   ConvShape cs{};              // OP_CONV
-  PoolShape ps{};              // pools; OP_FLATTEN uses N,C,H,W
+  PoolShape ps{};              // pools; OP_FLATTEN and OP_GROUPNORM use N,C,H,W
+  int groups = 0;              // OP_GROUPNORM: scales at w_off, shifts at b_off
   int64_t w_off = 0, b_off = 0;
   int in_t = 0, out_t = 0;     // tensor indices
-  size_t arg_off = 0;          // byte offset of the max-pool argmax, from the workspace base
+  size_t arg_off = 0;          // byte offset of the max-pool argmax or the normalisation's statistics, from the workspace base
   // bf16 MFMA path (conv / fc ops that qualify)
   bool mfma = false;
   VConv vc{};
@@ -197,6 +199,51 @@ static const sasgd_layer kAlex8[] = {
     {SASGD_FC, 4096, 0, 0, 0},  {SASGD_RELU, 0, 0, 0, 0},
     {SASGD_FC, 1000, 0, 0, 0}};
 
+// ---- group normalisation: tensors are dense and 256-byte aligned, so whole 16 bytes wherever their channels are
+static GroupNormShape norm_shape(const Net* net, const Op& op) {
+  return GroupNormShape{op.ps.N, op.ps.H * op.ps.W, op.ps.C, op.groups, net->bf16};
+}
+static bool norm_wide(const Net* net, const Op& op) { return op.ps.C % (net->bf16 ? 8 : 4) == 0; }
+// Scratch that a call of `count` learners needs of each; *lanes: the largest launch.
+static size_t norm_scratch(const Net* net, const Op& op, int count, int64_t* lanes) {
+  const GroupNormShape s = norm_shape(net, op);
+  size_t most = 0;
+  for (int gradient = 0; gradient < 2; gradient++) {
+    const GroupNormPlan p = group_norm_plan(s, norm_wide(net, op), gradient != 0, count);
+    most = std::max(most, group_norm_scratch_bytes(s, p, gradient != 0));
+    *lanes = std::max(*lanes, count * (s.images + 7) * (p.whole ? p.slabs : p.chunks) * p.threads);
+  }
+  return most;
+}
+// Arguments that both passes share.
+static GroupNormArgs norm_args(const Net* net, const Op& op, const PtrTab& ws, const CPtrTab& wts, int count, bool gradient) {
+  GroupNormArgs a;
+  memset(&a, 0, sizeof(a));
+  const int size = net->bf16 ? 2 : 4;
+  for (int k = 0; k < count; k++) {
+    a.base[k] = (uintptr_t)ws.p[k];
+    a.wts[k] = (uintptr_t)wts.p[k];
+  }
+  a.s = norm_shape(net, op);
+  a.plan = group_norm_plan(a.s, norm_wide(net, op), gradient, count);
+  a.learners = count;
+  a.x = (int64_t)net->tensors[(size_t)op.in_t].off * size;
+  a.y = (int64_t)net->tensors[(size_t)op.out_t].off * size;
+  a.x_pixel = a.y_pixel = op.ps.C;
+  a.x_image = a.y_image = (int64_t)a.s.positions * op.ps.C;
+  a.stats = (int64_t)op.arg_off;
+  a.parts = (int64_t)net->scratch_off;
+  a.sums = a.parts + (int64_t)group_norm_sums_at(a.s, a.plan);
+  a.scale = op.w_off * size;
+  a.shift = op.b_off * size;
+  a.dscale = op.w_off * 4;
+  a.dshift = op.b_off * 4;
+  a.has_scale = a.has_shift = a.has_stats = 1;
+  a.param_bf16 = net->bf16;
+  a.eps = 1e-5f;
+  return a;
+}
+
 int net_create(const sasgd_config& cfg, Net** out, int64_t* out_P, size_t* out_pack_elems, std::string& err) {
   const sasgd_layer* layers = nullptr;
   int nl = 0, C = 0, H = 0, W = 0;
@@ -257,7 +304,7 @@ int net_create(const sasgd_config& cfg, Net** out, int64_t* out_P, size_t* out_p
   for (int li = 0; li < nl; li++) {
     const sasgd_layer& L = layers[li];
     if (L.kind == SASGD_RELU) {
-      if (net->ops.empty() || net->tensors[(size_t)cur].relu) { delete net; err = "relu must directly follow a conv, fc or pooling layer"; return SASGD_EINVAL; }
+      if (net->ops.empty() || net->tensors[(size_t)cur].relu) { delete net; err = "relu must directly follow a conv, fc, pooling or groupnorm layer"; return SASGD_EINVAL; }
       net->ops.back().relu = true;
       net->tensors[(size_t)cur].relu = true;
       continue;
@@ -312,6 +359,21 @@ int net_create(const sasgd_config& cfg, Net** out, int64_t* out_P, size_t* out_p
       H = op.ps.OH; W = op.ps.OW;
       cur = op.out_t = new_tensor((size_t)N * C * H * W);
       if (op.kind == OP_POOL_MAX) { op.arg_off = arg_bytes; arg_bytes += ((size_t)N * C * H * W + 255) & ~(size_t)255; }
+    } else if (L.kind == SASGD_GROUPNORM) {
+      if (L.units < 1 || C % L.units != 0 || C > (C % chunk == 0 ? kWideNormChannels : kNarrowNormChannels) || (int64_t)H * W > kNormPositions) {
+        delete net; err = "groupnorm layer: groups must divide the channels, at most 4096 (1024 where they are no whole 16 bytes)"; return SASGD_EINVAL;
+      }
+      op.kind = OP_GROUPNORM;
+      op.groups = L.units;
+      op.ps = PoolShape{N, C, H, W, H, W, 1, 1};
+      op.w_off = P;
+      P += C;
+      op.b_off = P;
+      P += C;
+      op.in_t = cur;
+      cur = op.out_t = new_tensor((size_t)N * C * H * W);
+      op.arg_off = arg_bytes;
+      arg_bytes += ((size_t)N * L.units * 8 + 255) & ~(size_t)255;
     } else if (L.kind == SASGD_FC) {
       if (L.units < 1) { delete net; err = "fc layer: bad shape"; return SASGD_EINVAL; }
       if (!flat && H * W > 1) {           // bring the tensor into the (C,H,W) order of the fc weights
@@ -500,6 +562,10 @@ int net_create(const sasgd_config& cfg, Net** out, int64_t* out_P, size_t* out_p
     }
     sb = std::max(sb, parts);
   }
+  int64_t lanes = 0;
+  for (const Op& op : net->ops)             // (how a call is cut goes by its learners)
+    for (int count = 1; op.kind == OP_GROUPNORM && count <= cfg.lambda; count++) sb = std::max(sb, norm_scratch(net, op, count, &lanes));
+  if (lanes >= ((int64_t)1 << 32)) { delete net; err = "groupnorm layer: too many images of all learners"; return SASGD_ERANGE; }
   if (sb > 0) {
     net->scratch_off = (bytes + 255) & ~(size_t)255;
     net->scratch_bytes = sb;
@@ -793,6 +859,12 @@ hipError_t net_calc_gradient(Net* net, const int* learners, const LearnerBind* b
       case OP_POOL_AVG:
         TRY(launch_pool_fwd(bf, op.kind == OP_POOL_MAX, ws, xi, yo, op.arg_off, op.ps, op.relu, T[(size_t)op.in_t].relu, count, stream));
         break;
+      case OP_GROUPNORM: {
+        GroupNormArgs a = norm_args(net, op, ws, wts, count, false);
+        a.activation = op.relu ? SASGD_ACT_RELU : SASGD_ACT_NONE;
+        TRY(launch_group_norm(a, stream));
+        break;
+      }
       case OP_FLATTEN:
         TRY(launch_flatten_fwd(bf, ws, xi, yo, op.ps.N, op.ps.C, op.ps.H, op.ps.W, count, stream));
         break;
@@ -908,6 +980,17 @@ hipError_t net_calc_gradient(Net* net, const int* learners, const LearnerBind* b
       case OP_POOL_AVG:
         if (need_dx) TRY(launch_pool_bwd(bf, op.kind == OP_POOL_MAX, ws, dy, dx, op.arg_off, op.ps, tin.relu, tin.off, count, stream));
         break;
+      case OP_GROUPNORM: {                      // (what reaches dy has been masked by the output's ReLU)
+        GroupNormArgs a = norm_args(net, op, ws, wts, count, true);
+        for (int l = 0; l < count; l++) a.grads[l] = (uintptr_t)grads.p[l];
+        a.dy = (int64_t)dy * (bf ? 2 : 4);
+        a.dx = (int64_t)dx * (bf ? 2 : 4);
+        a.has_dx = need_dx;
+        a.mask = tin.relu;
+        a.has_dscale = a.has_dshift = 1;
+        TRY(launch_group_norm_gradient(a, stream));
+        break;
+      }
       case OP_FLATTEN:
         if (need_dx) TRY(launch_flatten_bwd(bf, ws, dy, dx, op.ps.N, op.ps.C, op.ps.H, op.ps.W, tin.relu, tin.off, count, stream));
         break;

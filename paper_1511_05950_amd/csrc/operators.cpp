@@ -33,12 +33,10 @@ inline int64_t blocks_of(int64_t numel) { return (numel + kMomentBlock - 1) / kM
 constexpr int64_t kMostElements = (int64_t)1 << 34;     // of a tensor and of a call: its launch stays below 2^32 lanes
 
 // ---------------------------------------------------------------- group normalisation
-constexpr int kWideChannels = 4096, kNarrowChannels = 1024;   // sums by channel of a workgroup lie in LDS
-
 const char* shape_error(const sasgd_norm_shape* s) {
   if (!s) return "null shape";
-  if (s->images < 0 || s->positions < 1 || s->positions > ((int64_t)1 << 26)) return "images or positions out of range";
-  if (s->channels < 1 || s->channels > kWideChannels || s->groups < 1 || s->channels % s->groups != 0) return "channels must be 1..4096 and a multiple of groups";
+  if (s->images < 0 || s->positions < 1 || s->positions > kNormPositions) return "images or positions out of range";
+  if (s->channels < 1 || s->channels > kWideNormChannels || s->groups < 1 || s->channels % s->groups != 0) return "channels must be 1..4096 and a multiple of groups";
   if ((s->type != SASGD_FP32 && s->type != SASGD_BF16) || (s->param_type != SASGD_FP32 && s->param_type != SASGD_BF16)) return "unknown type";
   if (s->activation < SASGD_ACT_NONE || s->activation > SASGD_ACT_SILU) return "unknown activation";
   if (!(s->eps > 0.f && s->eps < INFINITY)) return "eps must be positive and finite";
@@ -48,12 +46,6 @@ const char* shape_error(const sasgd_norm_shape* s) {
 }
 
 GroupNormShape inner_shape(const sasgd_norm_shape& s) { return GroupNormShape{s.images, (int)s.positions, s.channels, s.groups, s.type == SASGD_BF16}; }
-
-size_t align16(size_t n) { return (n + 15) & ~(size_t)15; }
-
-size_t need_bytes(const GroupNormShape& s, const GroupNormPlan& p, bool gradient) {
-  return align16(group_norm_part_bytes(s, p)) + (gradient ? group_norm_sum_bytes(s, p) : 0);
-}
 
 // Checks what both directions have in common and fills the launch's arguments; nullptr if all is well.
 const char* group_norm_args(const sasgd_norm_shape* shape, const void* x, const void* y, const void* dx, const void* scale, const void* shift,
@@ -79,16 +71,16 @@ const char* group_norm_args(const sasgd_norm_shape* shape, const void* x, const 
   if (((uintptr_t)scale | (uintptr_t)shift) & (psize - 1)) return "scale and shift must be aligned to their elements";
   const int vec = 16 / size;
   const bool wide = (low & 15) == 0 && (a.s.channels | a.x_pixel | a.y_pixel | a.x_image | a.y_image) % vec == 0;
-  if (!wide && a.s.channels > kNarrowChannels) return "more than 1024 channels must be whole 16 bytes, in strides and pointers too";
+  if (!wide && a.s.channels > kNarrowNormChannels) return "more than 1024 channels must be whole 16 bytes, in strides and pointers too";
   a.plan = group_norm_plan(a.s, wide, gradient, 1);
   if ((a.s.images + 8) * (int64_t)(a.plan.whole ? a.plan.slabs : a.plan.chunks) * a.plan.threads >= ((int64_t)1 << 32)) return "too many images for a launch";
-  const size_t need = need_bytes(a.s, a.plan, gradient);
+  const size_t need = group_norm_scratch_bytes(a.s, a.plan, gradient);
   if (need > 0 && (!work || ((uintptr_t)work & 15) || work_bytes < need)) return "workspace missing, too small or not 16-byte aligned";
   a.x = (int64_t)(uintptr_t)x;
   (gradient ? a.dy : a.y) = (int64_t)(uintptr_t)y;
   a.dx = (int64_t)(uintptr_t)dx;
   a.parts = (int64_t)(uintptr_t)work;
-  a.sums = a.parts + (int64_t)align16(group_norm_part_bytes(a.s, a.plan));
+  a.sums = a.parts + (int64_t)group_norm_sums_at(a.s, a.plan);
   a.scale = (int64_t)(uintptr_t)scale;
   a.shift = (int64_t)(uintptr_t)shift;
   a.has_scale = scale != nullptr;
@@ -107,8 +99,8 @@ int sasgd_groupNormWorkspace(const sasgd_norm_shape* shape, int32_t gradient, si
   size_t most = 0;
   for (int wide = 0; wide < 2; wide++) {
     if (wide && s.channels % (s.bf16 ? 8 : 4) != 0) continue;
-    if (!wide && s.channels > kNarrowChannels) continue;
-    most = std::max(most, need_bytes(s, group_norm_plan(s, wide != 0, gradient != 0, 1), gradient != 0));
+    if (!wide && s.channels > kNarrowNormChannels) continue;
+    most = std::max(most, group_norm_scratch_bytes(s, group_norm_plan(s, wide != 0, gradient != 0, 1), gradient != 0));
   }
   *out_bytes = most;
   return SASGD_OK;

@@ -96,8 +96,11 @@ struct GroupNormArgs {
   FastDiv by_cpg;            // of channel numbers, up to 4096: exact
   int32_t spread;            // lanes that add one group's chunks in the second launch, a power of two
 };
-size_t group_norm_part_bytes(const GroupNormShape& s, const GroupNormPlan& p);
-size_t group_norm_sum_bytes(const GroupNormShape& s, const GroupNormPlan& p);
+// Scratch of a learner: chunks' statistics, then (from group_norm_sums_at on) the gradient's channel sums.
+size_t group_norm_sums_at(const GroupNormShape& s, const GroupNormPlan& p);
+size_t group_norm_scratch_bytes(const GroupNormShape& s, const GroupNormPlan& p, bool gradient);
+constexpr int kWideNormChannels = 4096, kNarrowNormChannels = 1024;   // sums by channel of a workgroup lie in LDS; narrow: not moved 16 bytes at a time
+constexpr int64_t kNormPositions = (int64_t)1 << 26;
 hipError_t launch_group_norm(GroupNormArgs& a, hipStream_t stream);
 hipError_t launch_group_norm_gradient(GroupNormArgs& a, hipStream_t stream);
 

@@ -10,6 +10,7 @@ Network descriptions are plain tuples:
     ("maxpool", k, stride)           ceil-mode window, clipped at the border
     ("avgpool", k, stride)           same geometry, mean over in-bounds elements
     ("relu",)
+    ("groupnorm", groups)            group normalisation: a scale and a shift per channel
     ("fc", out)                      fully connected with bias (input flattened C,H,W)
 The loss (softmax cross-entropy, mean over the mini-batch) is implied after the last layer.
 
@@ -84,7 +85,7 @@ def _pool_out(n, k, s):
 
 
 def param_shapes(net):
-    """[(weight_shape, bias_len)] for every conv/fc layer, in network order."""
+    """[(weight_shape, bias_len)] for every layer with parameters, in network order (a normalisation's scales and shifts)."""
     c, h, w = net["input"]
     out = []
     for L in net["layers"]:
@@ -97,6 +98,8 @@ def param_shapes(net):
         elif L[0] in ("maxpool", "avgpool"):
             _, k, s = L
             h, w = _pool_out(h, k, s), _pool_out(w, k, s)
+        elif L[0] == "groupnorm":
+            out.append(((c,), c))
         elif L[0] == "fc":
             out.append(((L[1], c * h * w), L[1]))
             c, h, w = L[1], 1, 1
@@ -109,11 +112,11 @@ def num_params(net):
 
 # --------------------------------------------------------------------------- draws
 def init_weights(net, seed, std=0.01):
-    """Flat fp32 parameter vector: per layer Gaussian(0, std) weights then zero biases."""
+    """Flat fp32 parameter vector: per layer Gaussian(0, std) weights then zero biases; around 1 for a normalisation's scales."""
     rng = np.random.default_rng(seed)
     parts = []
     for ws, b in param_shapes(net):
-        parts.append((rng.standard_normal(int(np.prod(ws))) * std).astype(np.float32))
+        parts.append((rng.standard_normal(int(np.prod(ws))) * std + (1.0 if len(ws) == 1 else 0.0)).astype(np.float32))
         parts.append(np.zeros(b, np.float32))
     return np.concatenate(parts)
 
