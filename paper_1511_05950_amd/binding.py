@@ -363,15 +363,15 @@ def _place(stream):
 _fast_knows_torch = []
 
 
-def _want(name, t, types, numel=None):
-    """A contiguous tensor of one of the types (their names) on the current device, of at least `numel` elements where that is given."""
+def _want(name, t, types, numel):
+    """A contiguous tensor of one of the types (their names) on the current device, of at least `numel` elements."""
     if t.get_device() != _place(0)[0]:
         raise ValueError(name + " is not on the current device")
     if str(t.dtype)[6:] not in types:
         raise TypeError("%s must be %s, not %s" % (name, " or ".join(types), t.dtype))
     if not t.is_contiguous():
         raise ValueError(name + " must be contiguous")
-    if numel is not None and t.numel() < numel:
+    if t.numel() < numel:
         raise ValueError("%s has %d elements, %d are needed" % (name, t.numel(), numel))
 
 
@@ -438,21 +438,13 @@ class AdamW:
 
     def __init__(self, weights, m, v, m_scale=None, v_scale=None, copies=None, outs=None, alpha0=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
                  weight_decay=0.0, lr_mode="per_gradient", seed=0):
-        load()
+        device, _ = _place(0)
         weights = list(weights)
         n = len(weights)
         outs = weights if outs is None else list(outs)
         copies = [None] * n if copies is None else list(copies)
-        if len(outs) != n or len(copies) != n:
-            raise ValueError("outs and copies need an entry per tensor")
-        elements = momentElements(weights)
         self._tensors = (SasgdTensor * max(1, n))()
-        for e, w, o, s in zip(self._tensors, weights, outs, copies):
-            _want("weights", w, ("float32",))
-            _want("outs", o, ("float32",), w.numel())
-            if s is not None:
-                _want("copies", s, ("bfloat16",), w.numel())
-            e.numel, e.theta_in, e.theta_out, e.shadow_out = w.numel(), _addr(w), _addr(o), _addr(s)
+        elements = _fast.adamw_tensors(weights, outs, copies, device, ctypes.addressof(self._tensors))
         self._moments, small = _moments(m, v, m_scale, v_scale, elements)
         self._rule = SasgdAdamw(LR_MODES[lr_mode] if isinstance(lr_mode, str) else lr_mode, MOMENTS_E4M3 if small else MOMENTS_FP32, FP32,
                                 seed & 0xFFFFFFFF, alpha0, beta1, beta2, eps, weight_decay)

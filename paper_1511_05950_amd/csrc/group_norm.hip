@@ -51,9 +51,47 @@ __device__ __forceinline__ void pack(bf16_t& r, const float (&f)[1]) { r = f2bf(
 // 1 / (1 + exp(-z)) by the hardware's exponential and reciprocal (1 ulp each)
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f)); }
 
+// Past the caches: what a call reads or writes for the last time.  (Segments of 48 bytes of a line that several workgroups share then take twice as long:
+// group_norm_plan cuts channels at 64 bytes.  AlexNet-shaped second layer's gradient 100 -> 90 us, 2 304 x 32 x 32 x 32 behind silu 116 -> 105, 288 x
+// 54 x 54 x 96 forward 105 -> 91.)
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ float4 load_once(const float4* p) {
+  const f4 v = __builtin_nontemporal_load((const f4*)p);
+  return make_float4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+  const u4 v = __builtin_nontemporal_load((const u4*)p);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ float load_once(const float* p) { return *p; }
+__device__ __forceinline__ bf16_t load_once(const bf16_t* p) { return *p; }
+__device__ __forceinline__ void store_once(float4* p, const float4& r) {
+  const f4 v = {r.x, r.y, r.z, r.w};
+  __builtin_nontemporal_store(v, (f4*)p);
+}
+__device__ __forceinline__ void store_once(uint4* p, const uint4& r) {
+  const u4 v = {r.x, r.y, r.z, r.w};
+  __builtin_nontemporal_store(v, (u4*)p);
+}
+__device__ __forceinline__ void store_once(float* p, float r) { *p = r; }
+__device__ __forceinline__ void store_once(bf16_t* p, bf16_t r) { *p = r; }
+// N vectors of a lane, `step` apart, those from `count` on left out.
+template <bool ONCE, int N, typename R, typename T>
+__device__ __forceinline__ void load_rows(R (&held)[N], const T* x, int64_t step, int count) {
+#pragma unroll
+  for (int k = 0; k < N; k++)
+    if (k < count) held[k] = ONCE ? load_once((const R*)(x + k * step)) : *(const R*)(x + k * step);
+}
+template <bool ONCE, typename R>
+__device__ __forceinline__ void store_row(R* p, const R& r) {
+  if (ONCE) store_once(p, r);
+  else *p = r;
+}
+
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
-  if (ACT == SASGD_ACT_RELU) return z <= 0.f ? 0.f : z;         // (NaN stays)
+  if (ACT == SASGD_ACT_RELU) return __builtin_elementwise_maximum(z, 0.f);       // (NaN stays)
   if (ACT == SASGD_ACT_SILU) return z * sigmoid(z);
   return z;
 }
@@ -83,6 +121,23 @@ __device__ __forceinline__ float param(const GroupNormArgs& A, uintptr_t at, int
 }
 
 constexpr int kLaneChannels = 64;    // channels of a group up to which one lane adds them
+
+// Scales and shifts of the workgroup's channels, a lane a channel, to LDS: a lane has its eight from there instead of sixteen loads of its own (behind
+// the next barrier).  Fetched in front of the values and written behind them: what waits for them does not wait for the values.
+struct Params {
+  uint32_t scale, shift;
+  __device__ __forceinline__ void fetch(const GroupNormArgs& A, uintptr_t wts, int c) {
+    const uintptr_t a = wts + A.scale, b = wts + A.shift;
+    scale = shift = 0;
+    if (A.has_scale) scale = A.param_bf16 ? ((const bf16_t*)a)[c] : ((const uint32_t*)a)[c];
+    if (A.has_shift) shift = A.param_bf16 ? ((const bf16_t*)b)[c] : ((const uint32_t*)b)[c];
+  }
+  __device__ __forceinline__ void put(const GroupNormArgs& A, float* to_scale, float* to_shift) const {
+    const int up = A.param_bf16 ? 16 : 0;
+    *to_scale = A.has_scale ? __uint_as_float(scale << up) : 1.f;
+    *to_shift = __uint_as_float(shift << up);
+  }
+};
 
 // Which image of a learner, and which slab of its channels or chunk of its positions, a workgroup works on.  Parts of one image are eight
 // workgroups apart: they run on one XCD at about the same time, where narrow slabs share the lines of L2.
@@ -171,34 +226,36 @@ __device__ __forceinline__ void row_sums(const GroupNormCols& cols, int n, float
   __syncthreads();
 }
 
-// Mean and sum of squared distances of every channel of `np` positions from what lanes have of them: lane sums `sum` of `count` values and
-// squared distances `dev` from the lane's own mean.  mean[c], dev[c]; rows: 2 threads V floats, red: threads floats.
-template <int V>
-__device__ __forceinline__ void channel_moments(const float (&sum)[V], const float (&dev)[V], const GroupNormCols& cols, const Lanes& l, int np, float* rows,
-                                                float* red, float* mean, float* m2) {
-  const int n = cols.cols * V;
+// Sums of a vector's values go by units of V / U neighbouring channels: all of a group's, or as many as divide it (U = 1, V / 2 or V).
+// Mean and sum of squared distances of every unit of `np` positions from what lanes have of them: lane sums `sum` and squared distances `dev` from the
+// lane's own mean.  mean[c], dev[c]; rows: 2 threads U floats, red: threads floats.
+template <int V, int U>
+__device__ __forceinline__ void unit_moments(const float (&sum)[U], const float (&dev)[U], const GroupNormCols& cols, const Lanes& l, int np, float* rows,
+                                             float* red, float* mean, float* m2) {
+  const int n = cols.cols * U;
   float* rd = rows + cols.rows * n;
   if (l.active)
 #pragma unroll
-    for (int j = 0; j < V; j++) {
-      rows[l.row * n + l.col * V + j] = sum[j];
-      rd[l.row * n + l.col * V + j] = dev[j];
+    for (int j = 0; j < U; j++) {
+      rows[l.row * n + l.col * U + j] = sum[j];
+      rd[l.row * n + l.col * U + j] = dev[j];
     }
   __syncthreads();
   row_sums<1>(cols, n, red, mean, 0, [&](int, int r, int c) { return rows[r * n + c]; });
-  const float inv = 1.f / (float)np;
+  constexpr int kEach = V / U;
+  const float inv = 1.f / (float)(np * kEach);
   for (int c = threadIdx.x; c < n; c += blockDim.x) mean[c] *= inv;
   __syncthreads();
   // a row has its share of the positions, the first ones one more
   const int each = np / cols.rows, more = np - each * cols.rows;
-  const float one = each > 0 ? 1.f / (float)each : 0.f, plus = 1.f / (float)(each + 1);
+  const float one = each > 0 ? 1.f / (float)(each * kEach) : 0.f, plus = 1.f / (float)((each + 1) * kEach);
   row_sums<1>(cols, n, red, m2, 0, [&](int, int r, int c) {
-    const float count = (float)(each + (r < more)), off = rows[r * n + c] * (r < more ? plus : one) - mean[c];
+    const float count = (float)((each + (r < more)) * kEach), off = rows[r * n + c] * (r < more ? plus : one) - mean[c];
     return rd[r * n + c] + (count > 0.f ? count * off * off : 0.f);
   });
 }
 
-// The workgroup's groups from the moments of their channels (mean[c], m2[c] of `np` values each): done(g, mean, sum of squared distances).  A lane a
+// The workgroup's groups from the moments of their `cpg` units (mean[c], m2[c] of `np` values each): done(g, mean, sum of squared distances).  A lane a
 // group, or a wavefront a group where they have many channels (320 channels in 32 groups by wavefronts: 4 us of a workgroup's 9).
 template <typename F>
 __device__ __forceinline__ void group_moments(const float* mean, const float* m2, int groups, int cpg, int np, F done) {
@@ -230,33 +287,106 @@ __device__ __forceinline__ void group_moments(const float* mean, const float* m2
   }
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void add_moments(const typename Raw<T, V>::type& raw, const float (&first)[V], float (&s)[V], float (&q)[V]) {
+// What a lane adds up of its positions.  Distances from the lane's first value: the cancellation costs at most as many roundings of the
+// result as there are values, as none is further from their mean than the root of that many variances.
+template <typename T, int V, int U>
+struct Moments {
+  float first[V], s[V], q[V];
+  __device__ __forceinline__ void start(const typename Raw<T, V>::type& raw, bool any) {
+#pragma unroll
+    for (int j = 0; j < V; j++) first[j] = s[j] = q[j] = 0.f;
+    if (any) unpack(raw, first);
+    if (U < V)
+#pragma unroll
+      for (int j = 0; j < V; j++) first[j] = first[j / (V / U) * (V / U)];
+    if (U < V && any) add(raw);
+  }
+  __device__ __forceinline__ void add(const typename Raw<T, V>::type& raw) {
+    float f[V];
+    unpack(raw, f);
+#pragma unroll
+    for (int j = 0; j < V; j++) {
+      const float e = f[j] - first[j];
+      s[j] += e;
+      q[j] = fmaf(e, e, q[j]);
+    }
+  }
+  // sum and squared distances of the lane's mean, by units, of `count` positions; false: not to the precision wanted
+  __device__ __forceinline__ bool close(int count, float (&sum)[U], float (&dev)[U]) const {
+    constexpr int kEach = V / U;
+    const float n = (float)(count * kEach), inv = count > 0 ? 1.f / n : 0.f;
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      float a = 0.f, b = 0.f;
+#pragma unroll
+      for (int j = k * kEach; j < (k + 1) * kEach; j++) {
+        a += s[j];
+        b += q[j];
+      }
+      dev[k] = fmaxf(b - a * a * inv, 0.f);
+      sum[k] = count > 0 ? fmaf(first[k * kEach], n, a) : 0.f;
+    }
+    return true;
+  }
+};
+// bf16 in units of two channels and more: pairs by the dot product instructions, one instruction a value instead of four.  Distances from 0, so
+// where a lane's values are far from 0 against their spread its squared distances are added up again from its mean.
+template <int U>
+struct DotMoments {
+  float s[4], q[4];
+  __device__ __forceinline__ void start(const uint4& raw, bool any) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) s[j] = q[j] = 0.f;
+    if (any) add(raw);
+  }
+  __device__ __forceinline__ void add(const uint4& raw) {
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    const bf2 ones = __builtin_bit_cast(bf2, 0x3f803f80u);
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      const bf2 x = __builtin_bit_cast(bf2, w[k]);
+      s[k] = __builtin_amdgcn_fdot2_f32_bf16(x, ones, s[k], false);
+      q[k] = __builtin_amdgcn_fdot2_f32_bf16(x, x, q[k], false);
+    }
+  }
+  __device__ __forceinline__ bool close(int count, float (&sum)[U], float (&dev)[U]) const {
+    constexpr int kEach = 4 / U;
+    const float inv = count > 0 ? 1.f / (float)(count * 8 / U) : 0.f;
+    bool fine = true;
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      float a = 0.f, b = 0.f;
+#pragma unroll
+      for (int j = k * kEach; j < (k + 1) * kEach; j++) {
+        a += s[j];
+        b += q[j];
+      }
+      sum[k] = a;
+      dev[k] = fmaxf(b - a * a * inv, 0.f);
+      fine = fine && !(dev[k] < 0.125f * b);
+    }
+    return fine;
+  }
+};
+template <typename T, int V, int U> using LaneMoments = std::conditional_t<(V == 8 && U < 8), DotMoments<U>, Moments<T, V, U>>;
+// Squared distances from the lane's means, once more.
+template <typename T, int V, int U>
+__device__ __forceinline__ void add_distances(const typename Raw<T, V>::type& raw, const float (&mean)[U], float (&dev)[U]) {
   float f[V];
   unpack(raw, f);
 #pragma unroll
   for (int j = 0; j < V; j++) {
-    const float e = f[j] - first[j];
-    s[j] += e;
-    q[j] = fmaf(e, e, q[j]);
-  }
-}
-// From sums of distances from the lane's first value to the sum and the squared distances from the lane's mean: the cancellation costs
-// at most `count` roundings of the result, as no value is further from the mean than the root of count variances.
-template <int V>
-__device__ __forceinline__ void close_moments(const float (&first)[V], float (&s)[V], float (&q)[V], int count) {
-  const float n = (float)count, inv = count > 0 ? 1.f / n : 0.f;
-#pragma unroll
-  for (int j = 0; j < V; j++) {
-    q[j] = fmaxf(q[j] - s[j] * s[j] * inv, 0.f);
-    s[j] = count > 0 ? fmaf(first[j], n, s[j]) : 0.f;
+    const float e = f[j] - mean[j / (V / U)];
+    dev[j / (V / U)] = fmaf(e, e, dev[j / (V / U)]);
   }
 }
 __device__ __forceinline__ int count_of(const Lanes& l, int np) { return l.active && l.row < np ? (np - 1 - l.row) / l.rows + 1 : 0; }
 
 // ------------------------------------------------------------------------------------------------ forward
-// A workgroup holds a slab of an image.  LDS: rows [2 threads V], red [threads], mean [S], m2 [S], group [2 S / cpg]
-template <typename T, int V, int NV, int ACT>
+// A workgroup holds a slab of an image.  LDS: scale [S], shift [S], rows [2 threads U], red [threads], mean and m2 of the
+// units, group [2 S / cpg]
+template <typename T, int V, int U, int NV, int ACT, bool ONCE>
 __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_norm_kernel(const GroupNormArgs A) {
   extern __shared__ float lds[];
   typedef typename Raw<T, V>::type raw_t;
@@ -267,37 +397,45 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
   const int c0 = at.part * A.plan.slab, S = min(A.plan.slab, C - c0), np = A.s.positions;
   const GroupNormCols cols = A.cols[at.part == A.plan.slabs - 1];
   const int t = threadIdx.x, threads = blockDim.x;
-  float* rows = lds;
-  float* red = rows + 2 * threads * V;
+  float* scale = lds;
+  float* rows = scale + 2 * S;
+  float* red = rows + 2 * threads * U;
   float* mean = red + threads;
-  float* m2 = mean + S;
-  float* group = m2 + S;
+  float* m2 = mean + S / (V / U);
+  float* group = m2 + S / (V / U);
   const Lanes l = lanes_of(cols, t);
   const int count = count_of(l, np), first_c = l.col * V;
   const T* x = (const T*)(base + A.x) + at.image * A.x_image + l.row * A.x_pixel + c0 + first_c;
   const int64_t step = l.rows * A.x_pixel;
+  Params par;
+  if (t < S) par.fetch(A, wts, c0 + t);
   raw_t held[NV];
-#pragma unroll
-  for (int k = 0; k < NV; k++)
-    if (k < count) held[k] = *(const raw_t*)(x + k * step);
-  float sc[V], sh[V];
-#pragma unroll
-  for (int j = 0; j < V; j++) {
-    sc[j] = A.has_scale && l.active ? param(A, wts + A.scale, c0 + first_c + j) : 1.f;
-    sh[j] = A.has_shift && l.active ? param(A, wts + A.shift, c0 + first_c + j) : 0.f;
+  load_rows<ONCE>(held, x, step, count);
+  for (int c = t; c < S; c += threads) {
+    if (c != t) par.fetch(A, wts, c0 + c);
+    par.put(A, scale + c, scale + S + c);
   }
   {
-    float first[V], s[V], q[V];
-#pragma unroll
-    for (int j = 0; j < V; j++) first[j] = s[j] = q[j] = 0.f;
-    if (count > 0) unpack(held[0], first);
+    LaneMoments<T, V, U> mom;
+    float sum[U], dev[U];
+    mom.start(held[0], count > 0);
 #pragma unroll
     for (int k = 1; k < NV; k++)
-      if (k < count) add_moments<T, V>(held[k], first, s, q);
-    close_moments<V>(first, s, q, count);
-    channel_moments<V>(s, q, cols, l, np, rows, red, mean, m2);
+      if (k < count) mom.add(held[k]);
+    if (!mom.close(count, sum, dev)) {
+      float mu[U];
+#pragma unroll
+      for (int j = 0; j < U; j++) {
+        mu[j] = sum[j] / (float)(count * (V / U));
+        dev[j] = 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < NV; k++)
+        if (k < count) add_distances<T, V, U>(held[k], mu, dev);
+    }
+    unit_moments<V, U>(sum, dev, cols, l, np, rows, red, mean, m2);
   }
-  group_moments(mean, m2, A.by_cpg(S), cpg, np, [&](int g, float mu, float sq) {
+  group_moments(mean, m2, A.by_cpg(S), cpg / (V / U), np * (V / U), [&](int g, float mu, float sq) {
     const float r = 1.f / sqrtf(sq / ((float)np * (float)cpg) + A.eps);
     group[2 * g] = mu;
     group[2 * g + 1] = r;
@@ -305,13 +443,22 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
   });
   __syncthreads();
   if (count == 0) return;
-  float mu[V], r[V], slope[V];
+  float mu[V], slope[V], sh[V];
+  if (V > 1) {                                       // (S is whole vectors: 16-byte places)
+#pragma unroll
+    for (int j = 0; j < V; j += 4) {
+      *(float4*)(slope + j) = *(const float4*)(scale + first_c + j);
+      *(float4*)(sh + j) = *(const float4*)(scale + S + first_c + j);
+    }
+  } else {
+    slope[0] = scale[first_c];
+    sh[0] = scale[S + first_c];
+  }
 #pragma unroll
   for (int j = 0; j < V; j++) {
-    const int g = A.by_cpg(first_c + j);
+    const int g = A.by_cpg(first_c + (U == 1 ? 0 : j));
     mu[j] = group[2 * g];
-    r[j] = group[2 * g + 1];
-    slope[j] = r[j] * sc[j];
+    slope[j] *= group[2 * g + 1];
   }
   T* y = (T*)(base + A.y) + at.image * A.y_image + l.row * A.y_pixel + c0 + first_c;
   const int64_t ystep = l.rows * A.y_pixel;
@@ -321,15 +468,16 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
       float f[V];
       unpack(held[k], f);
 #pragma unroll
-      for (int j = 0; j < V; j++) f[j] = activate<ACT>(affine<ACT>(f[j] - mu[j], r[j], sc[j], slope[j], sh[j]));
+      for (int j = 0; j < V; j++) f[j] = activate<ACT>(fmaf(f[j] - mu[j], slope[j], sh[j]));
       raw_t o;
       pack(o, f);
-      *(raw_t*)(y + k * ystep) = o;
+      store_row<ONCE>((raw_t*)(y + k * ystep), o);
     }
 }
 
-// Images that no workgroup can hold, first launch: the moments of a chunk of positions.  LDS: rows, red, mean [C], m2 [C]
-template <typename T, int V>
+// Images that no workgroup can hold, first launch: the moments of a chunk of positions.  LDS: rows [2 threads U], red [threads], mean and m2 of the units
+constexpr int kAhead = 8;            // loads of a lane on their way
+template <typename T, int V, int U>
 __global__ __launch_bounds__(256) void group_norm_chunk_kernel(const GroupNormArgs A) {
   extern __shared__ float lds[];
   typedef typename Raw<T, V>::type raw_t;
@@ -339,9 +487,9 @@ __global__ __launch_bounds__(256) void group_norm_chunk_kernel(const GroupNormAr
   const int C = A.s.channels, cpg = A.cpg, p0 = at.part * A.plan.chunk, np = min(A.plan.chunk, A.s.positions - p0);
   const int t = threadIdx.x, threads = blockDim.x;
   float* rows = lds;
-  float* red = rows + 2 * threads * V;
+  float* red = rows + 2 * threads * U;
   float* mean = red + threads;
-  float* m2 = mean + C;
+  float* m2 = mean + C / (V / U);
   const T* x0 = (const T*)(base + A.x) + at.image * A.x_image + (int64_t)p0 * A.x_pixel;
   for (int c0 = 0; c0 < C; c0 += A.cols[0].cols * V) {      // (one turn up to `threads` vectors a pixel)
     const GroupNormCols cols = A.cols[c0 + A.cols[0].cols * V >= C];
@@ -349,28 +497,62 @@ __global__ __launch_bounds__(256) void group_norm_chunk_kernel(const GroupNormAr
     const int count = count_of(l, np);
     const T* x = x0 + l.row * A.x_pixel + c0 + l.col * V;
     const int64_t step = l.rows * A.x_pixel;
-    float first[V], s[V], q[V];
+    LaneMoments<T, V, U> mom;
+    float sum[U], dev[U];
+    for (int k = 0; k < count || k == 0; k += kAhead) {
+      raw_t in[kAhead];
+      load_rows<false>(in, x + k * step, step, count - k);
+      if (k == 0) mom.start(in[0], count > 0);
 #pragma unroll
-    for (int j = 0; j < V; j++) first[j] = s[j] = q[j] = 0.f;
-    if (count > 0) unpack(*(const raw_t*)x, first);
-    int k = 1;
-    constexpr int U = 8;
-    for (; k + U <= count; k += U) {
-      raw_t in[U];
-#pragma unroll
-      for (int i = 0; i < U; i++) in[i] = *(const raw_t*)(x + (k + i) * step);
-#pragma unroll
-      for (int i = 0; i < U; i++) add_moments<T, V>(in[i], first, s, q);
+      for (int i = 0; i < kAhead; i++)
+        if (k + i < count && k + i > 0) mom.add(in[i]);
     }
-    for (; k < count; k++) add_moments<T, V>(*(const raw_t*)(x + k * step), first, s, q);
-    close_moments<V>(first, s, q, count);
-    channel_moments<V>(s, q, cols, l, np, rows, red, mean + c0, m2 + c0);
+    if (!mom.close(count, sum, dev)) {
+      float mu[U];
+#pragma unroll
+      for (int j = 0; j < U; j++) {
+        mu[j] = sum[j] / (float)(count * (V / U));
+        dev[j] = 0.f;
+      }
+      for (int k = 0; k < count; k++) add_distances<T, V, U>(*(const raw_t*)(x + k * step), mu, dev);
+    }
+    unit_moments<V, U>(sum, dev, cols, l, np, rows, red, mean + c0 / (V / U), m2 + c0 / (V / U));
   }
   float2* parts = (float2*)(base + A.parts) + (at.image * A.plan.chunks + at.part) * A.s.groups;
-  group_moments(mean, m2, A.s.groups, cpg, np, [&](int g, float mu, float sq) { parts[g] = make_float2(mu, sq); });
+  group_moments(mean, m2, A.s.groups, cpg / (V / U), np * (V / U), [&](int g, float mu, float sq) { parts[g] = make_float2(mu, sq); });
 }
 
-// Second launch: the image's statistics from its chunks', then y.  LDS: group [2 groups]
+// group[2 g], group[2 g + 1]: sums over the image's chunks of value(chunk, group), `spread` lanes a group (neighbouring lanes have neighbouring groups).
+// LDS: group [2 groups], then [2 spread groups].
+template <typename F>
+__device__ __forceinline__ void chunk_sums(float* group, int G, int chunks, int spread, F value) {
+  float2* part = (float2*)(group + 2 * G);
+  const int t = threadIdx.x, T = blockDim.x;
+  for (int i = t; i < G * spread; i += T) {
+    const int s = i / G, g = i - s * G;
+    float2 sum = make_float2(0.f, 0.f);
+#pragma unroll 4
+    for (int k = s; k < chunks; k += spread) {
+      const float2 v = value(k, g);
+      sum.x += v.x;
+      sum.y += v.y;
+    }
+    part[i] = sum;
+  }
+  __syncthreads();
+  for (int g = t; g < G; g += T) {
+    float2 sum = part[g];
+    for (int s = 1; s < spread; s++) {
+      sum.x += part[s * G + g].x;
+      sum.y += part[s * G + g].y;
+    }
+    group[2 * g] = sum.x;
+    group[2 * g + 1] = sum.y;
+  }
+  __syncthreads();
+}
+
+// Second launch: the image's statistics from its chunks', then y.  LDS: see chunk_sums
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(256) void group_norm_apply_kernel(const GroupNormArgs A) {
   extern __shared__ float group[];
@@ -383,38 +565,31 @@ __global__ __launch_bounds__(256) void group_norm_apply_kernel(const GroupNormAr
   const int t = threadIdx.x, threads = blockDim.x;
   const float2* parts = (const float2*)(base + A.parts) + at.image * chunks * G;
   const float last = (float)(A.s.positions - (chunks - 1) * chunk), full = (float)chunk, total = (float)A.s.positions, cpg = (float)A.cpg;
-  for (int i = t; i < G * A.spread; i += threads) {          // `spread` neighbouring lanes a group
-    const int g = i / A.spread, first = i - g * A.spread;
-    float s = 0.f, m2 = 0.f;
-    for (int k = first; k < chunks; k += A.spread) s += parts[k * G + g].x * (k < chunks - 1 ? full : last);
-    for (int o = 1; o < A.spread; o <<= 1) s += __shfl_xor(s, o, 64);
-    const float mu = s / total;
-    for (int k = first; k < chunks; k += A.spread) {
-      const float2 p = parts[k * G + g];
-      m2 += p.y + (k < chunks - 1 ? full : last) * cpg * (p.x - mu) * (p.x - mu);
-    }
-    for (int o = 1; o < A.spread; o <<= 1) m2 += __shfl_xor(m2, o, 64);
-    if (first == 0) {
-      const float r = 1.f / sqrtf(m2 / (total * cpg) + A.eps);
-      group[2 * g] = mu;
-      group[2 * g + 1] = r;
-      if (A.has_stats && at.part == 0) ((float2*)(base + A.stats))[at.image * G + g] = make_float2(mu, r);
-    }
+  // distances of the chunks' means from the first one's: sums of n d and of n d^2 + the chunks' own
+  chunk_sums(group, G, chunks, A.spread, [&](int k, int g) {
+    const float2 p = parts[k * G + g];
+    const float n = (k < chunks - 1 ? full : last), d = p.x - parts[g].x;
+    return make_float2(n * d, n * cpg * d * d + p.y);
+  });
+  for (int g = t; g < G; g += threads) {
+    const float s = group[2 * g] / total, m2 = fmaxf(group[2 * g + 1] - total * cpg * s * s, 0.f);
+    const float mu = parts[g].x + s, r = 1.f / sqrtf(m2 / (total * cpg) + A.eps);
+    group[2 * g] = mu;
+    group[2 * g + 1] = r;
+    if (A.has_stats && at.part == 0) ((float2*)(base + A.stats))[at.image * G + g] = make_float2(mu, r);
   }
   __syncthreads();
   for (int c0 = 0; c0 < C; c0 += A.cols[0].cols * V) {
     const Lanes l = lanes_of(A.cols[c0 + A.cols[0].cols * V >= C], t);
     const int count = count_of(l, np), c = c0 + l.col * V;
     if (count == 0) continue;
-    float mu[V], r[V], sc[V], sh[V], slope[V];
+    float mu[V], sh[V], slope[V];
 #pragma unroll
     for (int j = 0; j < V; j++) {
       const int g = A.by_cpg(c + j);
       mu[j] = group[2 * g];
-      r[j] = group[2 * g + 1];
-      sc[j] = A.has_scale ? param(A, wts + A.scale, c + j) : 1.f;
+      slope[j] = group[2 * g + 1] * (A.has_scale ? param(A, wts + A.scale, c + j) : 1.f);
       sh[j] = A.has_shift ? param(A, wts + A.shift, c + j) : 0.f;
-      slope[j] = r[j] * sc[j];
     }
     const T* x = (const T*)(base + A.x) + at.image * A.x_image + (int64_t)(p0 + l.row) * A.x_pixel + c;
     T* y = (T*)(base + A.y) + at.image * A.y_image + (int64_t)(p0 + l.row) * A.y_pixel + c;
@@ -423,21 +598,18 @@ __global__ __launch_bounds__(256) void group_norm_apply_kernel(const GroupNormAr
       float f[V];
       unpack(in, f);
 #pragma unroll
-      for (int j = 0; j < V; j++) f[j] = activate<ACT>(affine<ACT>(f[j] - mu[j], r[j], sc[j], slope[j], sh[j]));
+      for (int j = 0; j < V; j++) f[j] = activate<ACT>(fmaf(f[j] - mu[j], slope[j], sh[j]));
       raw_t o;
       pack(o, f);
-      *(raw_t*)(y + k * ystep) = o;
+      store_once((raw_t*)(y + k * ystep), o);
     };
-    constexpr int U = 4;
-    int k = 0;
-    for (; k + U <= count; k += U) {
-      raw_t in[U];
+    for (int k = 0; k < count; k += kAhead) {
+      raw_t in[kAhead];
+      load_rows<true>(in, x + k * step, step, count - k);
 #pragma unroll
-      for (int i = 0; i < U; i++) in[i] = *(const raw_t*)(x + (k + i) * step);
-#pragma unroll
-      for (int i = 0; i < U; i++) one(in[i], k + i);
+      for (int i = 0; i < kAhead; i++)
+        if (k + i < count) one(in[i], k + i);
     }
-    for (; k < count; k++) one(*(const raw_t*)(x + k * step), k);
   }
 }
 
@@ -489,17 +661,27 @@ __device__ __forceinline__ void gradient_sums(const float (&a)[V], const float (
   row_sums<2>(cols, n, red, out, stride, [&](int k, int r, int c) { return (k ? rb : rows)[r * n + c]; });
 }
 
-// s1 and s2 of the workgroup's groups from its channels' sums (the first is channel c0 of the image): done(g, s1, s2)
+// The workgroup's channel sums (`n` channels: sa of dz, sb of dz xhat) to `out`, then times scale(c) in place, for the groups' s1 and s2.
 template <typename F>
-__device__ __forceinline__ void group_gradient(const GroupNormArgs& A, uintptr_t wts, const float* sa, const float* sb, int c0, int groups, F done) {
-  const int t = threadIdx.x, T = blockDim.x, cpg = A.cpg;
+__device__ __forceinline__ void store_sums(float* sa, float* sb, int n, float2* out, F scale) {
+  for (int c = threadIdx.x; c < n; c += blockDim.x) {
+    const float w = scale(c);
+    out[c] = make_float2(sb[c], sa[c]);
+    sa[c] *= w;
+    sb[c] *= w;
+  }
+  __syncthreads();
+}
+// s1 and s2 of the workgroup's groups from those: done(g, s1, s2)
+template <typename F>
+__device__ __forceinline__ void group_gradient(const float* sa, const float* sb, int cpg, int groups, F done) {
+  const int t = threadIdx.x, T = blockDim.x;
   if (cpg <= kLaneChannels) {
     for (int g = t; g < groups; g += T) {
       float s1 = 0.f, s2 = 0.f;
       for (int c = g * cpg; c < (g + 1) * cpg; c++) {
-        const float w = A.has_scale ? param(A, wts + A.scale, c0 + c) : 1.f;
-        s1 = fmaf(w, sa[c], s1);
-        s2 = fmaf(w, sb[c], s2);
+        s1 += sa[c];
+        s2 += sb[c];
       }
       done(g, s1, s2);
     }
@@ -509,9 +691,8 @@ __device__ __forceinline__ void group_gradient(const GroupNormArgs& A, uintptr_t
   for (int g = t >> 6; g < groups; g += T >> 6) {
     float s1 = 0.f, s2 = 0.f;
     for (int c = g * cpg + lane; c < (g + 1) * cpg; c += 64) {
-      const float w = A.has_scale ? param(A, wts + A.scale, c0 + c) : 1.f;
-      s1 = fmaf(w, sa[c], s1);
-      s2 = fmaf(w, sb[c], s2);
+      s1 += sa[c];
+      s2 += sb[c];
     }
     s1 = wave_total(s1);
     s2 = wave_total(s2);
@@ -541,8 +722,8 @@ __device__ __forceinline__ void keep(uint4& r, const float (&f)[8]) {      // va
   r = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A workgroup holds a slab of x and dy.  LDS: rows [2 threads V], red [2 threads], sa [S], sb [S], group [2 S / cpg]
-template <typename T, int V, int NV, int ACT>
+// A workgroup holds a slab of x and dy.  LDS: scale [S], shift [S], rows [2 threads V], red [2 threads], sa [S], sb [S], group [2 S / cpg]
+template <typename T, int V, int NV, int ACT, bool ONCE>
 __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_norm_gradient_kernel(const GroupNormArgs A) {
   extern __shared__ float lds[];
   typedef typename Raw<T, V>::type raw_t;
@@ -553,7 +734,8 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
   const int c0 = at.part * A.plan.slab, S = min(A.plan.slab, C - c0), np = A.s.positions;
   const GroupNormCols cols = A.cols[at.part == A.plan.slabs - 1];
   const int t = threadIdx.x, threads = blockDim.x;
-  float* rows = lds;
+  float* scale = lds;
+  float* rows = scale + 2 * S;
   float* red = rows + 2 * threads * V;
   float* sums = red + 2 * threads;
   float* group = sums + 2 * S;
@@ -562,18 +744,46 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
   const T* x = (const T*)(base + A.x) + at.image * A.x_image + l.row * A.x_pixel + c0 + first_c;
   const T* dy = (const T*)(base + A.dy) + at.image * A.y_image + l.row * A.y_pixel + c0 + first_c;
   const int64_t step = l.rows * A.x_pixel, ystep = l.rows * A.y_pixel;
+  const int gs = A.by_cpg(S);
+  const float2* stats = (const float2*)(base + A.stats) + at.image * A.s.groups + A.by_cpg(c0);
+  Params par;
+  float2 stat = make_float2(0.f, 0.f);
+  if (t < S) par.fetch(A, wts, c0 + t);
+  if (t < gs) stat = stats[t];
   raw_t hx[NV];
   typename Kept<T, V, ACT>::type hz[NV];
   GradientLane<V> p;
   {
     raw_t hd[NV];
+    load_rows<ONCE>(hx, x, step, count);
+    load_rows<ONCE>(hd, dy, ystep, count);
+    for (int c = t; c < S; c += threads) {
+      if (c != t) par.fetch(A, wts, c0 + c);
+      par.put(A, scale + c, scale + S + c);
+    }
+    for (int g = t; g < gs; g += threads) {
+      if (g != t) stat = stats[g];
+      group[2 * g] = stat.x;
+      group[2 * g + 1] = stat.y;
+    }
+    __syncthreads();
+    if (V > 1) {                                     // (S is whole vectors: 16-byte places)
 #pragma unroll
-    for (int k = 0; k < NV; k++)
-      if (k < count) {
-        hx[k] = *(const raw_t*)(x + k * step);
-        hd[k] = *(const raw_t*)(dy + k * ystep);
+      for (int j = 0; j < V; j += 4) {
+        *(float4*)(p.sc + j) = *(const float4*)(scale + first_c + j);
+        *(float4*)(p.sh + j) = *(const float4*)(scale + S + first_c + j);
       }
-    if (l.active) load_lane<V>(A, base, wts, at.image, c0 + first_c, p);
+    } else {
+      p.sc[0] = scale[first_c];
+      p.sh[0] = scale[S + first_c];
+    }
+#pragma unroll
+    for (int j = 0; j < V; j++) {
+      const int g = A.by_cpg(first_c + j);
+      p.mu[j] = group[2 * g];
+      p.r[j] = group[2 * g + 1];
+      p.slope[j] = p.r[j] * p.sc[j];
+    }
     float a[V], b[V];
 #pragma unroll
     for (int j = 0; j < V; j++) a[j] = b[j] = 0.f;
@@ -588,12 +798,9 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
       }
     gradient_sums<V>(a, b, p, cols, l, rows, red, sums, S);
   }
-  {
-    float2* out = (float2*)(base + A.sums) + at.image * C + c0;
-    for (int c = t; c < S; c += threads) out[c] = make_float2(sums[S + c], sums[c]);
-  }
+  store_sums(sums, sums + S, S, (float2*)(base + A.sums) + at.image * C + c0, [&](int c) { return scale[c]; });
   if (!A.has_dx) return;
-  group_gradient(A, wts, sums, sums + S, c0, A.by_cpg(S), [&](int g, float s1, float s2) {
+  group_gradient(sums, sums + S, A.cpg, gs, [&](int g, float s1, float s2) {
     group[2 * g] = s1;
     group[2 * g + 1] = s2;
   });
@@ -621,7 +828,7 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
       }
       raw_t o;
       pack(o, d);
-      *(raw_t*)(dx + k * ystep) = o;
+      store_row<ONCE>((raw_t*)(dx + k * ystep), o);
     }
 }
 
@@ -657,29 +864,25 @@ __global__ __launch_bounds__(256) void group_norm_gradient_chunk_kernel(const Gr
       unpack(id, d);
       add_gradient<V, ACT>(f, d, p, a, b);
     };
-    constexpr int U = 4;
-    int k = 0;
-    for (; k + U <= count; k += U) {
-      raw_t ix[U], id[U];
+    constexpr int kPairs = kAhead / 2;
+    for (int k = 0; k < count; k += kPairs) {
+      raw_t ix[kPairs], id[kPairs];
+      load_rows<false>(ix, x + k * step, step, count - k);
+      load_rows<false>(id, dy + k * ystep, ystep, count - k);
 #pragma unroll
-      for (int i = 0; i < U; i++) {
-        ix[i] = *(const raw_t*)(x + (k + i) * step);
-        id[i] = *(const raw_t*)(dy + (k + i) * ystep);
-      }
-#pragma unroll
-      for (int i = 0; i < U; i++) one(ix[i], id[i]);
+      for (int i = 0; i < kPairs; i++)
+        if (k + i < count) one(ix[i], id[i]);
     }
-    for (; k < count; k++) one(*(const raw_t*)(x + k * step), *(const raw_t*)(dy + k * ystep));
     gradient_sums<V>(a, b, p, cols, l, rows, red, sa + c0, C);
   }
-  float2* out = (float2*)(base + A.sums) + (at.image * A.plan.chunks + at.part) * C;
-  for (int c = t; c < C; c += threads) out[c] = make_float2(sb[c], sa[c]);
+  store_sums(sa, sb, C, (float2*)(base + A.sums) + (at.image * A.plan.chunks + at.part) * C,
+             [&](int c) { return A.has_scale ? param(A, wts + A.scale, c) : 1.f; });
   if (!A.has_dx) return;
   float2* parts = (float2*)(base + A.parts) + (at.image * A.plan.chunks + at.part) * A.s.groups;
-  group_gradient(A, wts, sa, sb, 0, A.s.groups, [&](int g, float s1, float s2) { parts[g] = make_float2(s1, s2); });
+  group_gradient(sa, sb, A.cpg, A.s.groups, [&](int g, float s1, float s2) { parts[g] = make_float2(s1, s2); });
 }
 
-// Second launch: s1 and s2 of the image from its chunks', then dx.  LDS: group [2 groups]
+// Second launch: s1 and s2 of the image from its chunks', then dx.  LDS: see chunk_sums
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(256) void group_norm_gradient_apply_kernel(const GroupNormArgs A) {
   extern __shared__ float group[];
@@ -689,26 +892,10 @@ __global__ __launch_bounds__(256) void group_norm_gradient_apply_kernel(const Gr
   const uintptr_t base = A.base[blockIdx.y], wts = A.wts[blockIdx.y];
   const int C = A.s.channels, G = A.s.groups, chunks = A.plan.chunks;
   const int p0 = at.part * A.plan.chunk, np = min(A.plan.chunk, A.s.positions - p0);
-  const int t = threadIdx.x, threads = blockDim.x;
+  const int t = threadIdx.x;
   const float2* parts = (const float2*)(base + A.parts) + at.image * chunks * G;
   const float inv = 1.f / ((float)A.s.positions * (float)A.cpg);
-  for (int i = t; i < G * A.spread; i += threads) {
-    const int g = i / A.spread, first = i - g * A.spread;
-    float s1 = 0.f, s2 = 0.f;
-    for (int k = first; k < chunks; k += A.spread) {
-      s1 += parts[k * G + g].x;
-      s2 += parts[k * G + g].y;
-    }
-    for (int o = 1; o < A.spread; o <<= 1) {
-      s1 += __shfl_xor(s1, o, 64);
-      s2 += __shfl_xor(s2, o, 64);
-    }
-    if (first == 0) {
-      group[2 * g] = s1 * inv;
-      group[2 * g + 1] = s2 * inv;
-    }
-  }
-  __syncthreads();
+  chunk_sums(group, G, chunks, A.spread, [&](int k, int g) { return parts[k * G + g]; });
   for (int c0 = 0; c0 < C; c0 += A.cols[0].cols * V) {
     const Lanes l = lanes_of(A.cols[c0 + A.cols[0].cols * V >= C], t);
     const int count = count_of(l, np), ch = c0 + l.col * V;
@@ -719,8 +906,8 @@ __global__ __launch_bounds__(256) void group_norm_gradient_apply_kernel(const Gr
 #pragma unroll
     for (int j = 0; j < V; j++) {
       const int g = A.by_cpg(ch + j);
-      b[j] = -p.r[j] * group[2 * g];
-      c[j] = -p.r[j] * p.r[j] * group[2 * g + 1];
+      b[j] = -p.r[j] * (group[2 * g] * inv);
+      c[j] = -p.r[j] * p.r[j] * (group[2 * g + 1] * inv);
     }
     const T* x = (const T*)(base + A.x) + at.image * A.x_image + (int64_t)(p0 + l.row) * A.x_pixel + ch;
     const T* dy = (const T*)(base + A.dy) + at.image * A.y_image + (int64_t)(p0 + l.row) * A.y_pixel + ch;
@@ -739,36 +926,36 @@ __global__ __launch_bounds__(256) void group_norm_gradient_apply_kernel(const Gr
       }
       raw_t o;
       pack(o, d);
-      *(raw_t*)(dx + k * ystep) = o;
+      store_once((raw_t*)(dx + k * ystep), o);
     };
-    constexpr int U = 2;
-    int k = 0;
-    for (; k + U <= count; k += U) {
-      raw_t ix[U], id[U];
+    constexpr int kPairs = kAhead / 2;
+    for (int k = 0; k < count; k += kPairs) {
+      raw_t ix[kPairs], id[kPairs];
+      load_rows<true>(ix, x + k * step, step, count - k);
+      load_rows<true>(id, dy + k * ystep, ystep, count - k);
 #pragma unroll
-      for (int i = 0; i < U; i++) {
-        ix[i] = *(const raw_t*)(x + (k + i) * step);
-        id[i] = *(const raw_t*)(dy + (k + i) * ystep);
-      }
-#pragma unroll
-      for (int i = 0; i < U; i++) one(ix[i], id[i], k + i);
+      for (int i = 0; i < kPairs; i++)
+        if (k + i < count) one(ix[i], id[i], k + i);
     }
-    for (; k < count; k++) one(*(const raw_t*)(x + k * step), *(const raw_t*)(dy + k * ystep), k);
   }
 }
 
-// dscale, dshift: rows of channel sums [rows][C][2] added, 32 channels a workgroup and eight rows at a time.  Many rows in two launches: the first
-// leaves a row per blockIdx.y (`per` rows each).
+// dscale, dshift: rows of channel sums [rows][C][2] added, 32 channels a workgroup and 32 rows at a time.  Many rows in two launches: the first
+// leaves a row per blockIdx.y (`per` rows each).  256 rows 3 us, 2 304 in two launches 9; in one 28.
+#ifndef FROWS
+#define FROWS 512
+#endif
+constexpr int64_t kFinishRows = FROWS;
 template <bool LAST>
-__global__ __launch_bounds__(256) void group_norm_finish_kernel(const GroupNormArgs A, int64_t from, int64_t rows, int64_t per, int64_t to) {
-  __shared__ float2 part[8][32];
+__global__ __launch_bounds__(1024) void group_norm_finish_kernel(const GroupNormArgs A, int64_t from, int64_t rows, int64_t per, int64_t to) {
+  __shared__ float2 part[32][33];
   const int learner = blockIdx.z, ch = threadIdx.x & 31, seg = threadIdx.x >> 5, c = blockIdx.x * 32 + ch, C = A.s.channels;
   const int64_t r0 = blockIdx.y * per, r1 = r0 + per < rows ? r0 + per : rows;
   const float2* sums = (const float2*)(A.base[learner] + from);
   float a = 0.f, b = 0.f;
   if (c < C) {
 #pragma unroll 8
-    for (int64_t k = r0 + seg; k < r1; k += 8) {
+    for (int64_t k = r0 + seg; k < r1; k += 32) {
       const float2 s = sums[k * C + c];
       a += s.x;
       b += s.y;
@@ -776,41 +963,49 @@ __global__ __launch_bounds__(256) void group_norm_finish_kernel(const GroupNormA
   }
   part[seg][ch] = make_float2(a, b);
   __syncthreads();
-  if (seg == 0 && c < C) {
-    a = b = 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; k++) {
-      a += part[k][ch].x;
-      b += part[k][ch].y;
-    }
-    if (!LAST) {
-      ((float2*)(A.base[learner] + to))[(int64_t)blockIdx.y * C + c] = make_float2(a, b);
-    } else {
-      if (A.has_dscale) ((float*)(A.grads[learner] + A.dscale))[c] = a;
-      if (A.has_dshift) ((float*)(A.grads[learner] + A.dshift))[c] = b;
-    }
+  // a wavefront's halves take one channel each: its 32 rows
+  const int row = threadIdx.x & 31, own = threadIdx.x >> 5;
+  float2 s = part[row][own];
+  for (int o = 16; o > 0; o >>= 1) {
+    s.x += __shfl_xor(s.x, o, 64);
+    s.y += __shfl_xor(s.y, o, 64);
+  }
+  const int to_c = blockIdx.x * 32 + own;
+  if (row != 0 || to_c >= C) return;
+  if (!LAST) {
+    ((float2*)(A.base[learner] + to))[(int64_t)blockIdx.y * C + to_c] = s;
+  } else {
+    if (A.has_dscale) ((float*)(A.grads[learner] + A.dscale))[to_c] = s.x;
+    if (A.has_dshift) ((float*)(A.grads[learner] + A.dshift))[to_c] = s.y;
   }
 }
 
-constexpr int64_t kFinishRows = 128;               // rows of sums that one launch adds; more in two launches, of this many each
-
-int64_t finish_splits(int64_t rows) { return rows <= kFinishRows ? 0 : std::min<int64_t>((rows + 63) / 64, kFinishRows); }
+int64_t finish_splits(int64_t rows) { return rows <= kFinishRows ? 0 : std::min<int64_t>((rows + 127) / 128, kFinishRows); }
 
 size_t lds_bytes(const GroupNormArgs& a, bool gradient) {
   const int S = a.plan.whole ? a.plan.slab : a.s.channels, T = a.plan.threads;
-  return ((size_t)T * (2 * a.plan.vec + (gradient ? 2 : 1)) + 2 * S + (a.plan.whole ? 2 * (S / a.cpg) : 0)) * 4;
+  return ((size_t)T * (2 * a.plan.vec + (gradient ? 2 : 1)) + 2 * S + (a.plan.whole ? 2 * (S / a.cpg) + 2 * S : 0)) * 4;
 }
 
 }  // namespace
 
-constexpr int kHeldForward[] = {4, 8, 16, 24, 36}, kHeldBackward[] = {4, 8, 12, 16}, kHeldNarrow[] = {8, 24};
+constexpr int kHeldForward[] = {4, 8, 16, 24, 36}, kHeldBackward[] = {4, 8, 12, 16, 24}, kHeldNarrow[] = {8, 24};
 
-// Small images are held whole, in slabs of whole groups and whole vectors: the smallest that makes segments of 128 bytes a pixel, or 64 or 32
-// where no more fit in, or all channels; smaller ones still where the launch would otherwise have fewer workgroups than the chip has places.
-GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient, int learners) {
+// Small images are held whole, in slabs of whole groups and whole vectors: the smallest that makes segments of 128 bytes a pixel, or 64 where no more
+// fit in, or all channels; smaller ones still where the launch would otherwise have fewer workgroups than the chip has places.
+#ifndef PLENTY
+#define PLENTY 1024
+#endif
+constexpr int64_t kPlenty = PLENTY;
+// Bytes of x up to which workgroups share lines, which then go through the caches (lanes hold up to eight vectors): the other way is two launches
+// and, backward, those of the chunks' sums.
+constexpr int64_t kSharedForward = 8 << 20, kSharedGradient = 32 << 20;
+
+GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient, bool silu, int learners) {
   GroupNormPlan p;
   const int size = s.bf16 ? 2 : 4, cpg = s.channels / s.groups;
   p.vec = wide ? 16 / size : 1;
+  p.once = true;
   int unit = cpg;
   while (unit % p.vec != 0) unit += cpg;           // (ends: the channels are whole vectors)
   p.chunk = s.positions;
@@ -835,27 +1030,39 @@ GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient,
     }
     if (gradient) {
       for (int held : kHeldBackward)
-        if (fits(256, held)) return true;
+        if (held <= (silu && s.bf16 ? 16 : 24) && fits(256, held)) return true;
       return false;
     }
     for (int held : kHeldForward)
       if (fits(256, held)) return true;
     return false;
   };
-  for (int bytes = 128; bytes >= 32; bytes /= 2) {
+    const int64_t all = s.images * learners * s.positions * s.channels * size;
+  auto slabs = [&](int slab) { return s.images * learners * ((s.channels + slab - 1) / slab); };
+  auto shares_lines = [&](int slab) { return slab < s.channels && ((slab * size) % 64 != 0 || (s.channels * size) % 64 != 0); };
+  for (int bytes = 128; bytes >= 64; bytes /= 2) {
     int slab = std::min(s.channels, (bytes / size + unit - 1) / unit * unit);
-    while (slab > unit && s.images * learners * ((s.channels + slab - 1) / slab) < 512) slab = std::max(unit, slab / 2 / unit * unit);
-    if (take(slab)) return p;
+    // many small images: larger slabs while there are workgroups enough and a lane holds no more than eight vectors
+    while (slab < s.channels && slabs(slab * 2) >= kPlenty && (int64_t)std::min(slab * 2, s.channels) / p.vec * s.positions <= 256 * 8) slab = std::min(slab * 2, s.channels);
+    while (slab > unit && slabs(slab) < 512) {
+      const int less = std::max(unit, slab / 2 / unit * unit);
+      if (shares_lines(less) && all > (gradient ? kSharedGradient : kSharedForward)) break;
+      slab = less;
+    }
+    if (shares_lines(slab) && all > (gradient ? kSharedGradient : kSharedForward)) continue;
+    if (!take(slab)) continue;
+    p.once = !shares_lines(slab);
+    if (p.once || p.held <= 8) return p;
   }
   p.whole = false;
   p.slab = s.channels;
   p.slabs = 1;
   p.threads = 256;
   p.held = 0;
-  // chunks of 64 KiB, smaller ones where that makes fewer than 1 024 workgroups, at most 32 an image and at least 16 KiB
+  // chunks of 64 KiB, smaller ones where that makes fewer than 1 024 workgroups, at most 64 an image and at least 16 KiB
   const int64_t image = (int64_t)s.positions * s.channels * size, images = std::max<int64_t>(1, s.images * learners);
   int64_t chunks = std::max((image + 65535) / 65536, (1024 + images - 1) / images);
-  chunks = std::min(std::min(chunks, image / 16384), (int64_t)32);
+  chunks = std::min(std::min(chunks, image / 16384), (int64_t)64);
   chunks = std::max<int64_t>(1, chunks);
   p.chunk = (int)((s.positions + chunks - 1) / chunks);
   p.chunks = (s.positions + p.chunk - 1) / p.chunk;
@@ -874,7 +1081,7 @@ static uint32_t workgroups(const GroupNormArgs& a) {
 }
 
 // The columns of lanes: [0] of a full slab (or turn of channels), [1] of the last.
-static void set_columns(GroupNormArgs& a) {
+static void set_columns(GroupNormArgs& a, int units) {       // units: of a vector, that sums go by
   const int V = a.plan.vec, all = (a.plan.whole ? a.plan.slab : a.s.channels) / V, most = std::min(all, a.plan.threads);
   const int last = a.plan.whole ? (a.s.channels - (a.plan.slabs - 1) * a.plan.slab) / V : all - (all - 1) / most * most;
   for (int k = 0; k < 2; k++) {
@@ -882,53 +1089,65 @@ static void set_columns(GroupNormArgs& a) {
     c.cols = k ? last : most;
     c.rows = a.plan.threads / c.cols;
     c.by_cols.set(c.cols);
-    const int n = c.cols * V;
+    const int n = c.cols * units;
     c.segs = a.plan.threads / n;
     c.by_n.set(n);
     c.fold = n < 64 && (n & (n - 1)) == 0;
   }
   a.cpg = a.s.channels / a.s.groups;
   a.by_cpg.set(a.cpg);
-  for (a.spread = 1; a.spread < 64 && a.spread * 2 <= a.plan.chunks && a.spread * 2 * a.s.groups <= a.plan.threads;) a.spread *= 2;
+  for (a.spread = 1; a.spread * 2 <= a.plan.chunks && a.spread * 2 * a.s.groups <= a.plan.threads;) a.spread *= 2;
 }
 
 #define BY_ACTIVATION(launch)                                                  \
   (a.activation == SASGD_ACT_RELU ? launch(std::integral_constant<int, SASGD_ACT_RELU>()) \
    : a.activation == SASGD_ACT_SILU ? launch(std::integral_constant<int, SASGD_ACT_SILU>()) : launch(std::integral_constant<int, SASGD_ACT_NONE>()))
 
-template <typename T, int V, int NV>
+template <typename T, int V, int U, int NV>
 static void forward_held(const GroupNormArgs& a, dim3 grid, hipStream_t stream) {
-  auto launch = [&](auto act) { group_norm_kernel<T, V, NV, decltype(act)::value><<<grid, a.plan.threads, lds_bytes(a, false), stream>>>(a); };
+  auto launch = [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
+    if constexpr (NV <= 8 && V > 1)
+      if (!a.plan.once) return group_norm_kernel<T, V, U, NV, ACT, false><<<grid, a.plan.threads, lds_bytes(a, false), stream>>>(a);
+    group_norm_kernel<T, V, U, NV, ACT, true><<<grid, a.plan.threads, lds_bytes(a, false), stream>>>(a);
+  };
   BY_ACTIVATION(launch);
 }
 template <typename T, int V, int NV>
 static void backward_held(const GroupNormArgs& a, dim3 grid, hipStream_t stream) {
-  auto launch = [&](auto act) { group_norm_gradient_kernel<T, V, NV, decltype(act)::value><<<grid, a.plan.threads, lds_bytes(a, true), stream>>>(a); };
+  auto launch = [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
+    if constexpr (NV <= 8 && V > 1)
+      if (!a.plan.once) return group_norm_gradient_kernel<T, V, NV, ACT, false><<<grid, a.plan.threads, lds_bytes(a, true), stream>>>(a);
+    // (behind silu dz of bf16 is kept in 32 bits: up to 16 vectors, group_norm_plan)
+    if constexpr (!(NV > 16 && ACT == SASGD_ACT_SILU && V == 8)) group_norm_gradient_kernel<T, V, NV, ACT, true><<<grid, a.plan.threads, lds_bytes(a, true), stream>>>(a);
+  };
   BY_ACTIVATION(launch);
 }
 
-template <typename T, int V>
-static hipError_t forward(const GroupNormArgs& a, hipStream_t stream) {
+template <typename T, int V, int U>
+static hipError_t forward(GroupNormArgs& a, hipStream_t stream) {
+  set_columns(a, U);
   const dim3 grid(workgroups(a), (uint32_t)a.learners);
   if (a.plan.whole) {
     if constexpr (V == 1) {
-      if (a.plan.held == 8) forward_held<T, V, 8>(a, grid, stream);
-      else forward_held<T, V, 24>(a, grid, stream);
+      if (a.plan.held == 8) forward_held<T, V, U, 8>(a, grid, stream);
+      else forward_held<T, V, U, 24>(a, grid, stream);
     } else {
       switch (a.plan.held) {
-        case 4: forward_held<T, V, 4>(a, grid, stream); break;
-        case 8: forward_held<T, V, 8>(a, grid, stream); break;
-        case 16: forward_held<T, V, 16>(a, grid, stream); break;
-        case 24: forward_held<T, V, 24>(a, grid, stream); break;
-        default: forward_held<T, V, 36>(a, grid, stream); break;
+        case 4: forward_held<T, V, U, 4>(a, grid, stream); break;
+        case 8: forward_held<T, V, U, 8>(a, grid, stream); break;
+        case 16: forward_held<T, V, U, 16>(a, grid, stream); break;
+        case 24: forward_held<T, V, U, 24>(a, grid, stream); break;
+        default: forward_held<T, V, U, 36>(a, grid, stream); break;
       }
     }
     return hipGetLastError();
   }
-  group_norm_chunk_kernel<T, V><<<grid, a.plan.threads, lds_bytes(a, false), stream>>>(a);
+  group_norm_chunk_kernel<T, V, U><<<grid, a.plan.threads, lds_bytes(a, false), stream>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  auto launch = [&](auto act) { group_norm_apply_kernel<T, V, decltype(act)::value><<<grid, a.plan.threads, (size_t)a.s.groups * 8, stream>>>(a); };
+  auto launch = [&](auto act) { group_norm_apply_kernel<T, V, decltype(act)::value><<<grid, a.plan.threads, (size_t)a.s.groups * (1 + a.spread) * 8, stream>>>(a); };
   BY_ACTIVATION(launch);
   return hipGetLastError();
 }
@@ -945,7 +1164,8 @@ static hipError_t backward(const GroupNormArgs& a, hipStream_t stream) {
         case 4: backward_held<T, V, 4>(a, grid, stream); break;
         case 8: backward_held<T, V, 8>(a, grid, stream); break;
         case 12: backward_held<T, V, 12>(a, grid, stream); break;
-        default: backward_held<T, V, 16>(a, grid, stream); break;
+        case 16: backward_held<T, V, 16>(a, grid, stream); break;
+        default: backward_held<T, V, 24>(a, grid, stream); break;
       }
     }
     return hipGetLastError();
@@ -954,22 +1174,24 @@ static hipError_t backward(const GroupNormArgs& a, hipStream_t stream) {
   BY_ACTIVATION(sums);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.has_dx) return e;
-  auto launch = [&](auto act) { group_norm_gradient_apply_kernel<T, V, decltype(act)::value><<<grid, a.plan.threads, (size_t)a.s.groups * 8, stream>>>(a); };
+  auto launch = [&](auto act) { group_norm_gradient_apply_kernel<T, V, decltype(act)::value><<<grid, a.plan.threads, (size_t)a.s.groups * (1 + a.spread) * 8, stream>>>(a); };
   BY_ACTIVATION(launch);
   return hipGetLastError();
 }
 
 hipError_t launch_group_norm(GroupNormArgs& a, hipStream_t stream) {
   if (a.s.images == 0) return hipSuccess;
-  set_columns(a);
-  if (a.s.bf16) return a.plan.vec == 8 ? forward<bf16_t, 8>(a, stream) : forward<bf16_t, 1>(a, stream);
-  return a.plan.vec == 4 ? forward<float, 4>(a, stream) : forward<float, 1>(a, stream);
+  const int cpg = a.s.channels / a.s.groups;
+  if (a.s.bf16 && a.plan.vec == 8) return cpg % 8 == 0 ? forward<bf16_t, 8, 1>(a, stream) : cpg % 2 == 0 ? forward<bf16_t, 8, 4>(a, stream) : forward<bf16_t, 8, 8>(a, stream);
+  if (a.s.bf16) return forward<bf16_t, 1, 1>(a, stream);
+  if (a.plan.vec == 4) return cpg % 4 == 0 ? forward<float, 4, 1>(a, stream) : forward<float, 4, 4>(a, stream);
+  return forward<float, 1, 1>(a, stream);
 }
 
 hipError_t launch_group_norm_gradient(GroupNormArgs& a, hipStream_t stream) {
   hipError_t e = hipSuccess;
   if (a.s.images > 0) {
-    set_columns(a);
+    set_columns(a, a.plan.vec);
     if (a.s.bf16) e = a.plan.vec == 8 ? backward<bf16_t, 8>(a, stream) : backward<bf16_t, 1>(a, stream);
     else e = a.plan.vec == 4 ? backward<float, 4>(a, stream) : backward<float, 1>(a, stream);
   }
@@ -979,13 +1201,13 @@ hipError_t launch_group_norm_gradient(GroupNormArgs& a, hipStream_t stream) {
   int64_t from = a.sums, left = rows;
   if (splits > 0) {
     const int64_t to = a.sums + rows * a.s.channels * 8, per = (rows + splits - 1) / splits;
-    group_norm_finish_kernel<false><<<dim3(strips, (uint32_t)splits, learners), 256, 0, stream>>>(a, from, rows, per, to);
+    group_norm_finish_kernel<false><<<dim3(strips, (uint32_t)splits, learners), 1024, 0, stream>>>(a, from, rows, per, to);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     from = to;
     left = splits;
   }
-  group_norm_finish_kernel<true><<<dim3(strips, 1, learners), 256, 0, stream>>>(a, from, left, left, 0);
+  group_norm_finish_kernel<true><<<dim3(strips, 1, learners), 1024, 0, stream>>>(a, from, left, left, 0);
   return hipGetLastError();
 }
 

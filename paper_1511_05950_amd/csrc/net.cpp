@@ -209,7 +209,7 @@ static size_t norm_scratch(const Net* net, const Op& op, int count, int64_t* lan
   const GroupNormShape s = norm_shape(net, op);
   size_t most = 0;
   for (int gradient = 0; gradient < 2; gradient++) {
-    const GroupNormPlan p = group_norm_plan(s, norm_wide(net, op), gradient != 0, count);
+    const GroupNormPlan p = group_norm_plan(s, norm_wide(net, op), gradient != 0, false, count);
     most = std::max(most, group_norm_scratch_bytes(s, p, gradient != 0));
     *lanes = std::max(*lanes, count * (s.images + 7) * (p.whole ? p.slabs : p.chunks) * p.threads);
   }
@@ -225,7 +225,7 @@ static GroupNormArgs norm_args(const Net* net, const Op& op, const PtrTab& ws, c
     a.wts[k] = (uintptr_t)wts.p[k];
   }
   a.s = norm_shape(net, op);
-  a.plan = group_norm_plan(a.s, norm_wide(net, op), gradient, count);
+  a.plan = group_norm_plan(a.s, norm_wide(net, op), gradient, false, count);
   a.learners = count;
   a.x = (int64_t)net->tensors[(size_t)op.in_t].off * size;
   a.y = (int64_t)net->tensors[(size_t)op.out_t].off * size;

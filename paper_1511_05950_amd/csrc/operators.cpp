@@ -72,7 +72,7 @@ const char* group_norm_args(const sasgd_norm_shape* shape, const void* x, const 
   const int vec = 16 / size;
   const bool wide = (low & 15) == 0 && (a.s.channels | a.x_pixel | a.y_pixel | a.x_image | a.y_image) % vec == 0;
   if (!wide && a.s.channels > kNarrowNormChannels) return "more than 1024 channels must be whole 16 bytes, in strides and pointers too";
-  a.plan = group_norm_plan(a.s, wide, gradient, 1);
+  a.plan = group_norm_plan(a.s, wide, gradient, a.activation == SASGD_ACT_SILU, 1);
   if ((a.s.images + 8) * (int64_t)(a.plan.whole ? a.plan.slabs : a.plan.chunks) * a.plan.threads >= ((int64_t)1 << 32)) return "too many images for a launch";
   const size_t need = group_norm_scratch_bytes(a.s, a.plan, gradient);
   if (need > 0 && (!work || ((uintptr_t)work & 15) || work_bytes < need)) return "workspace missing, too small or not 16-byte aligned";
@@ -100,7 +100,8 @@ int sasgd_groupNormWorkspace(const sasgd_norm_shape* shape, int32_t gradient, si
   for (int wide = 0; wide < 2; wide++) {
     if (wide && s.channels % (s.bf16 ? 8 : 4) != 0) continue;
     if (!wide && s.channels > kNarrowNormChannels) continue;
-    most = std::max(most, group_norm_scratch_bytes(s, group_norm_plan(s, wide != 0, gradient != 0, 1), gradient != 0));
+    for (int silu = 0; silu < 2; silu++)
+      most = std::max(most, group_norm_scratch_bytes(s, group_norm_plan(s, wide != 0, gradient != 0, silu != 0, 1), gradient != 0));
   }
   *out_bytes = most;
   return SASGD_OK;

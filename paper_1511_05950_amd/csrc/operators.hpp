@@ -63,13 +63,14 @@ struct GroupNormPlan {
   bool whole;      // a workgroup holds all positions of `slab` channels; otherwise it walks `chunk` positions of all channels, in two launches
   int slab, slabs;
   int chunk, chunks;
+  bool once;       // the tensors go past the caches
 };
 struct GroupNormShape {
   int64_t images;            // of a learner
   int positions, channels, groups;
   bool bf16;
 };
-GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient, int learners);
+GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient, bool silu, int learners);
 
 // How a workgroup's lanes lie over a pixel's channels: `cols` vectors side by side, `rows` pixels at a time; n = cols x vec channels.
 struct GroupNormCols {

@@ -440,6 +440,39 @@ static PyObject* gradient_norm(PyObject* self, PyObject* const* a, Py_ssize_t na
   Py_RETURN_NONE;
 }
 
+/* adamw_tensors(weights, outs, copies, device, tensors): fills the array of sasgd_tensor at `tensors` from lists of one length (an entry of copies may be
+ * None); returns how many elements their moments have. */
+static PyObject* adamw_tensors(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  int32_t device;
+  void* to;
+  int64_t elements_ = 0;
+  Py_ssize_t n, k;
+  NARGS(5);
+  if (integer32(a[3], &device) || address(a[4], &to)) return NULL;
+  if (!PyList_Check(a[0]) || !PyList_Check(a[1]) || !PyList_Check(a[2])) return PyErr_Format(PyExc_TypeError, "lists are needed");
+  n = PyList_GET_SIZE(a[0]);
+  if (PyList_GET_SIZE(a[1]) != n || PyList_GET_SIZE(a[2]) != n) return PyErr_Format(PyExc_ValueError, "outs and copies need an entry per tensor");
+  for (k = 0; k < n; k++) {
+    sasgd_tensor* t = (sasgd_tensor*)to + k;
+    view w, o, c;
+    if (want(PyList_GET_ITEM(a[0], k), "a weight", device, SASGD_FP32, 0, &w)) return NULL;
+    t->numel = elements(&w);
+    t->theta_in = (const float*)w.data;
+    t->theta_out = (float*)w.data;
+    t->shadow_out = NULL;
+    if (PyList_GET_ITEM(a[1], k) != PyList_GET_ITEM(a[0], k)) {
+      if (want(PyList_GET_ITEM(a[1], k), "an out", device, SASGD_FP32, t->numel, &o)) return NULL;
+      t->theta_out = (float*)o.data;
+    }
+    if (PyList_GET_ITEM(a[2], k) != Py_None) {
+      if (want(PyList_GET_ITEM(a[2], k), "a copy", device, SASGD_BF16, t->numel, &c)) return NULL;
+      t->shadow_out = (uint16_t*)c.data;
+    }
+    elements_ += (t->numel + 255) / 256 * 256;
+  }
+  return PyLong_FromLongLong(elements_);
+}
+
 /* apply_adamw(rule, tensors, count, moments, grads, staleness, step, step_dev, factor, device, stream): rule, tensors and moments are addresses of the
  * C structures, grads a sequence of c sequences of `count` tensors; the rule's grad_type becomes theirs. */
 static PyObject* apply_adamw(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
@@ -678,6 +711,7 @@ static PyMethodDef methods[] = {FAST(get_minibatch),
                                 FAST(calc_gradient),
                                 FAST(apply_update_no_alloc),
                                 FAST(gradient_norm),
+                                FAST(adamw_tensors),
                                 FAST(apply_adamw),
                                 FAST(group_norm_workspace),
                                 FAST(group_norm),
