@@ -563,6 +563,13 @@ __global__ __launch_bounds__(256) void group_norm_apply_kernel(const GroupNormAr
   const int C = A.s.channels, G = A.s.groups, chunk = A.plan.chunk, chunks = A.plan.chunks;
   const int p0 = at.part * chunk, np = min(chunk, A.s.positions - p0);
   const int t = threadIdx.x, threads = blockDim.x;
+  // the first values are on their way while the statistics are put together
+  const T* xp = (const T*)(base + A.x) + at.image * A.x_image + (int64_t)p0 * A.x_pixel;
+  raw_t in[kAhead];
+  {
+    const Lanes l = lanes_of(A.cols[A.cols[0].cols * V >= C], t);
+    load_rows<true>(in, xp + l.row * A.x_pixel + l.col * V, l.rows * A.x_pixel, count_of(l, np));
+  }
   const float2* parts = (const float2*)(base + A.parts) + at.image * chunks * G;
   const float last = (float)(A.s.positions - (chunks - 1) * chunk), full = (float)chunk, total = (float)A.s.positions, cpg = (float)A.cpg;
   // distances of the chunks' means from the first one's: sums of n d and of n d^2 + the chunks' own
@@ -591,7 +598,7 @@ __global__ __launch_bounds__(256) void group_norm_apply_kernel(const GroupNormAr
       slope[j] = group[2 * g + 1] * (A.has_scale ? param(A, wts + A.scale, c + j) : 1.f);
       sh[j] = A.has_shift ? param(A, wts + A.shift, c + j) : 0.f;
     }
-    const T* x = (const T*)(base + A.x) + at.image * A.x_image + (int64_t)(p0 + l.row) * A.x_pixel + c;
+    const T* x = xp + l.row * A.x_pixel + c;
     T* y = (T*)(base + A.y) + at.image * A.y_image + (int64_t)(p0 + l.row) * A.y_pixel + c;
     const int64_t step = l.rows * A.x_pixel, ystep = l.rows * A.y_pixel;
     auto one = [&](const raw_t& in, int k) {
@@ -604,8 +611,7 @@ __global__ __launch_bounds__(256) void group_norm_apply_kernel(const GroupNormAr
       store_once((raw_t*)(y + k * ystep), o);
     };
     for (int k = 0; k < count; k += kAhead) {
-      raw_t in[kAhead];
-      load_rows<true>(in, x + k * step, step, count - k);
+      if (k > 0 || c0 > 0) load_rows<true>(in, x + k * step, step, count - k);
 #pragma unroll
       for (int i = 0; i < kAhead; i++)
         if (k + i < count) one(in[i], k + i);
@@ -893,6 +899,17 @@ __global__ __launch_bounds__(256) void group_norm_gradient_apply_kernel(const Gr
   const int C = A.s.channels, G = A.s.groups, chunks = A.plan.chunks;
   const int p0 = at.part * A.plan.chunk, np = min(A.plan.chunk, A.s.positions - p0);
   const int t = threadIdx.x;
+  // the first values are on their way while the sums are put together
+  constexpr int kPairs = kAhead / 2;
+  const T* xp = (const T*)(base + A.x) + at.image * A.x_image + (int64_t)p0 * A.x_pixel;
+  const T* dp = (const T*)(base + A.dy) + at.image * A.y_image + (int64_t)p0 * A.y_pixel;
+  raw_t ix[kPairs], id[kPairs];
+  {
+    const Lanes l = lanes_of(A.cols[A.cols[0].cols * V >= C], t);
+    const int count = count_of(l, np);
+    load_rows<true>(ix, xp + l.row * A.x_pixel + l.col * V, l.rows * A.x_pixel, count);
+    load_rows<true>(id, dp + l.row * A.y_pixel + l.col * V, l.rows * A.y_pixel, count);
+  }
   const float2* parts = (const float2*)(base + A.parts) + at.image * chunks * G;
   const float inv = 1.f / ((float)A.s.positions * (float)A.cpg);
   chunk_sums(group, G, chunks, A.spread, [&](int k, int g) { return parts[k * G + g]; });
@@ -909,8 +926,8 @@ __global__ __launch_bounds__(256) void group_norm_gradient_apply_kernel(const Gr
       b[j] = -p.r[j] * (group[2 * g] * inv);
       c[j] = -p.r[j] * p.r[j] * (group[2 * g + 1] * inv);
     }
-    const T* x = (const T*)(base + A.x) + at.image * A.x_image + (int64_t)(p0 + l.row) * A.x_pixel + ch;
-    const T* dy = (const T*)(base + A.dy) + at.image * A.y_image + (int64_t)(p0 + l.row) * A.y_pixel + ch;
+    const T* x = xp + l.row * A.x_pixel + ch;
+    const T* dy = dp + l.row * A.y_pixel + ch;
     T* dx = (T*)(base + A.dx) + at.image * A.y_image + (int64_t)(p0 + l.row) * A.y_pixel + ch;
     const int64_t step = l.rows * A.x_pixel, ystep = l.rows * A.y_pixel;
     auto one = [&](const raw_t& ix, const raw_t& id, int k) {
@@ -928,11 +945,11 @@ __global__ __launch_bounds__(256) void group_norm_gradient_apply_kernel(const Gr
       pack(o, d);
       store_once((raw_t*)(dx + k * ystep), o);
     };
-    constexpr int kPairs = kAhead / 2;
     for (int k = 0; k < count; k += kPairs) {
-      raw_t ix[kPairs], id[kPairs];
-      load_rows<true>(ix, x + k * step, step, count - k);
-      load_rows<true>(id, dy + k * ystep, ystep, count - k);
+      if (k > 0 || c0 > 0) {
+        load_rows<true>(ix, x + k * step, step, count - k);
+        load_rows<true>(id, dy + k * ystep, ystep, count - k);
+      }
 #pragma unroll
       for (int i = 0; i < kPairs; i++)
         if (k + i < count) one(ix[i], id[i], k + i);
@@ -942,10 +959,7 @@ __global__ __launch_bounds__(256) void group_norm_gradient_apply_kernel(const Gr
 
 // dscale, dshift: rows of channel sums [rows][C][2] added, 32 channels a workgroup and 32 rows at a time.  Many rows in two launches: the first
 // leaves a row per blockIdx.y (`per` rows each).  256 rows 3 us, 2 304 in two launches 9; in one 28.
-#ifndef FROWS
-#define FROWS 512
-#endif
-constexpr int64_t kFinishRows = FROWS;
+constexpr int64_t kFinishRows = 512;
 template <bool LAST>
 __global__ __launch_bounds__(1024) void group_norm_finish_kernel(const GroupNormArgs A, int64_t from, int64_t rows, int64_t per, int64_t to) {
   __shared__ float2 part[32][33];
@@ -993,10 +1007,7 @@ constexpr int kHeldForward[] = {4, 8, 16, 24, 36}, kHeldBackward[] = {4, 8, 12, 
 
 // Small images are held whole, in slabs of whole groups and whole vectors: the smallest that makes segments of 128 bytes a pixel, or 64 where no more
 // fit in, or all channels; smaller ones still where the launch would otherwise have fewer workgroups than the chip has places.
-#ifndef PLENTY
-#define PLENTY 1024
-#endif
-constexpr int64_t kPlenty = PLENTY;
+constexpr int64_t kPlenty = 1024;
 // Bytes of x up to which workgroups share lines, which then go through the caches (lanes hold up to eight vectors): the other way is two launches
 // and, backward, those of the chunks' sums.
 constexpr int64_t kSharedForward = 8 << 20, kSharedGradient = 32 << 20;
