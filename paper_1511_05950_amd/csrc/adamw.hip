@@ -160,7 +160,7 @@ __device__ __forceinline__ void adamw_blocks(const AdamwLaunch& A, const AdamwSt
     constexpr int kAhead = R == 1 ? 8 : 2;
 #pragma unroll kAhead
     for (int l = 1; l < A.c; l++) {
-      const G* gl = (const G*)w[A.grads_at + l] + at;
+      const G* gl = (const G*)(A.apart_at ? w[A.grads_at] + A.tab.word[A.apart_at + l] : w[A.grads_at + l]) + at;
       const float part = share[l];
       float t[R][4];
 #pragma unroll

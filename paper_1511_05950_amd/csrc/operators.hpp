@@ -23,9 +23,10 @@ struct TensorTable {
 constexpr uint64_t kAligned = (uint64_t)1 << 63;
 
 struct AdamwLaunch {
-  TensorTable tab;           // words of a tensor: numel, theta_in, [theta_out], [shadow], g_0 .. g_{c-1}; the c shares (float) come first
-  int32_t c, has_out, has_shadow, grads_at;   // grads_at: a tensor's word with g_0;  tensors' words begin behind the shares
+  TensorTable tab;           // words of a tensor: numel, theta_in, [theta_out], [shadow], g_0 .. g_{c-1}; the c shares (float) come first, then distances
+  int32_t c, has_out, has_shadow, grads_at;   // grads_at: a tensor's word with g_0;  tensors' words begin at words_at, behind the shares
   int32_t words_at;
+  int32_t apart_at;          // not 0: every gradient lies as far from g_0 in all tensors (flat vectors), by c words from here on; tensors have g_0 alone
   uint32_t seed;
   int64_t block0;            // moments' block of the launch's first block
   void* m;

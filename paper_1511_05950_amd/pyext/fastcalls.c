@@ -388,8 +388,13 @@ static int list_of(PyObject* seq, Py_ssize_t n, int device, int* kind, const voi
     if (v.kind == KIND_OTHER) return bad(PyExc_TypeError, "a gradient", "must be float32 or bfloat16");
     if (*kind == KIND_OTHER) *kind = v.kind;
     if (v.kind != *kind) return bad(PyExc_TypeError, "a gradient", "has another type than the first one");
-    if (!contiguous(&v)) return bad(PyExc_ValueError, "a gradient", "must be contiguous");
-    count = elements(&v);
+    if (v.dims == 1) {
+      count = v.shape[0];
+      if (count > 1 && v.stride[0] != 1) return bad(PyExc_ValueError, "a gradient", "must be contiguous");
+    } else {
+      count = elements(&v);
+      if (!contiguous(&v)) return bad(PyExc_ValueError, "a gradient", "must be contiguous");
+    }
     if (known && count != *at) return bad(PyExc_ValueError, "a gradient", "has not its tensor's length");
     if (!known) *at = count;
     data[(size_t)k * apart] = v.data;

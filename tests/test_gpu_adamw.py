@@ -224,6 +224,26 @@ def test_more_tensors_than_a_launch_takes(states):
     r.step(2)
 
 
+@pytest.mark.parametrize("states", ["fp32", "e4m3"])
+@pytest.mark.parametrize("c", [2, 7])
+def test_gradients_that_are_flat_vectors(c, states):
+    """Gradients cut alike out of flat vectors, at any distance from each other: the same bits as gradients that lie anywhere."""
+    a, b = (Run([7, 300, 0, 1025, 64] * 60, torch.float32, states, c, copies=False, seed=3) for _ in range(2))
+    total = sum(a.sizes)
+    buffers = [torch.zeros(total + 3 * l, device="cuda") for l in range(c)]
+    for l, flat in enumerate(buffers):
+        at, lists = 2 * l, []
+        for n, g in zip(b.sizes, b.lists[l]):
+            flat[at:at + n] = g
+            lists.append(flat[at:at + n])
+            at += n
+        b.lists[l] = lists
+    for t in (1, 2):
+        a.step(t)
+        b.step(t)
+    assert torch.equal(a.flat, b.flat) and torch.equal(a.m.view(torch.uint8), b.m.view(torch.uint8)) and torch.equal(a.v.view(torch.uint8), b.v.view(torch.uint8))
+
+
 @pytest.mark.parametrize("kw", [dict(beta1=0.0), dict(beta2=0.0), dict(beta1=0.0, beta2=0.0, eps=1.0), dict(wd=0.0, alpha0=0.0), dict(std=1e-12), dict(std=1e8)])
 @pytest.mark.parametrize("states", ["fp32", "e4m3"])
 def test_extreme_rules_and_gradients(states, kw):
