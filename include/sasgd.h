@@ -204,7 +204,8 @@ int sasgd_applyUpdateNoAlloc(const float* theta_in_dev, float* theta_out_dev, fl
  * `stream` (hipStream_t, NULL = default stream; it belongs to the current device), err / err_len an optional host buffer that
  * receives a message when a call fails.  They may be captured into a graph.  Calls that overlap in time must not share
  * moments or a workspace.  Pointers need the alignment of their elements only, the moments 16 bytes; where the weights, gradients
- * and copies of a tensor are 16-, 16- (bf16: 8-) and 8-byte aligned it is moved 16 bytes a lane. */
+ * and copies of a tensor are 16-, 16- (bf16: 8-) and 8-byte aligned it is moved 16 bytes a lane.
+ * What is written (weights, copies, moments, results) overlaps nothing else of a call: no tensor is listed twice. */
 
 /* gradientNorm: out_dev[0] = sqrt(sum over all tensors of g^2), squares and sums in 64 bits in a fixed order; out_dev[1] = the factor
  * that bounds the norm: 1 where max_norm is 0 or the norm is not above it, max_norm / norm beyond, NaN where the norm is not finite.
@@ -301,7 +302,7 @@ typedef struct {
 int sasgd_groupNormWorkspace(const sasgd_norm_shape* shape, int32_t gradient, size_t* out_bytes);
 
 /* groupNorm.  scale, shift: device [channels], or NULL for ones and zeros.  stats_dev: optional device float32 [images][groups][2], receives
- * mean and r, which the backward pass needs.  y_dev may be x_dev (with x's strides).  workspace_dev: 16-byte aligned, any contents.
+ * mean and r, which the backward pass needs.  y_dev may be x_dev (with x's strides); else what is written lies apart from what is read, here and below.  workspace_dev: 16-byte aligned, any contents.
  * Errors: EINVAL (argument), EHIP. */
 int sasgd_groupNorm(const sasgd_norm_shape* shape, const void* x_dev, const void* scale_dev, const void* shift_dev, void* y_dev, float* stats_dev,
                     void* workspace_dev, size_t workspace_bytes, void* stream, char* err, size_t err_len);
@@ -309,7 +310,8 @@ int sasgd_groupNorm(const sasgd_norm_shape* shape, const void* x_dev, const void
 /* groupNormGradient: with dz = dy act'(z) and xhat = (x - mean) r
  *     dshift = sum dz;   dscale = sum dz xhat   over images and positions, in a fixed order;
  *     dx = r (scale dz - (sum scale dz + xhat sum scale dz xhat) / m)   the sums over the group
- * z is computed again, with the rounding of the forward pass.  dx_dev, dscale_dev, dshift_dev (float32 [channels]): each optional; dx_dev may
+ * z is computed again: (x - mean) r, times scale, plus shift, each rounded (where |z| is a rounding or two the forward pass may have seen its
+ * other sign).  dx_dev, dscale_dev, dshift_dev (float32 [channels]): each optional; dx_dev may
  * be dy_dev.  No images: dscale and dshift become 0.  Errors: EINVAL (argument), EHIP. */
 int sasgd_groupNormGradient(const sasgd_norm_shape* shape, const void* x_dev, const void* scale_dev, const void* shift_dev, const float* stats_dev,
                             const void* dy_dev, void* dx_dev, float* dscale_dev, float* dshift_dev, void* workspace_dev, size_t workspace_bytes,

@@ -8,10 +8,16 @@
 // written, so where a workgroup can hold them in registers they are read once ("whole"); where it cannot, a first launch
 // leaves statistics of chunks of positions and a second one reads the values again (from the memory-side cache, as far as they fit).
 //
-// Sums go channel by channel: a lane owns 16 bytes of channels at a fixed place of the pixel and walks positions, the rows of lanes
-// are added through LDS in a fixed order, and groups are put together from their channels, whatever number of channels a group has.
-// Variances are sums of squared distances from the mean of what is summed, joined by
-// sum of those + sum of count x (mean - joint mean)^2, from lanes to channels to groups: no difference of large sums.
+// Sums go by units of neighbouring channels (one, two, or a lane's whole vector where a group is whole vectors; one in the backward pass, whose dscale
+// and dshift want them): a lane owns 16 bytes of channels at a fixed place of the pixel and walks positions, the rows of lanes are added through LDS in a
+// fixed order, and groups are put together from their units, whatever number of channels a group has.  Variances are sums of squared distances
+// from the mean of what is summed, joined by sum of those + sum of count x (mean - joint mean)^2, from lanes to units to groups: no difference of
+// large sums.
+//
+// What bounds it now (MI355X; a copy of these tensors runs at 4.7 TB/s): bf16 2 304 x 32 x 32 x 32 gradient 105 us, 4.3 TB/s; 288 x 27 x 27 x 256
+// gradient 78 us, 4.1 TB/s: HBM, and the vector ALU between the phases of a workgroup.  288 x 54 x 54 x 96 forward 96 us: 35 of statistics, 59 at the copy's
+// rate; held in slabs of 24 channels it was 106 (segments of 48 bytes of a line).  16 x 64 x 64 x 320 34 us: both launches' ends.  4 x 32 x 32 x 32
+// fp32 7 us: a launch and the chain of its phases.
 #include "dev_common.hpp"
 #include "operators.hpp"
 
@@ -52,8 +58,8 @@ __device__ __forceinline__ void pack(bf16_t& r, const float (&f)[1]) { r = f2bf(
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f)); }
 
 // Past the caches: what a call reads or writes for the last time.  (Segments of 48 bytes of a line that several workgroups share then take twice as long:
-// group_norm_plan cuts channels at 64 bytes.  AlexNet-shaped second layer's gradient 100 -> 90 us, 2 304 x 32 x 32 x 32 behind silu 116 -> 105, 288 x
-// 54 x 54 x 96 forward 105 -> 91.)
+// group_norm_plan cuts channels at 64 bytes.  Through them and past them, bf16: 288 x 27 x 27 x 256 gradient 91 and 78 us, 2 304 x 32 x 32 x 32 120 and 105,
+// 288 x 54 x 54 x 96 forward 114 and 94, 16 x 64 x 64 x 320 36 and 34.)
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ float4 load_once(const float4* p) {
@@ -95,8 +101,8 @@ __device__ __forceinline__ float activate(float z) {
   if (ACT == SASGD_ACT_SILU) return z * sigmoid(z);
   return z;
 }
-// z from x - mean.  Behind a ReLU each operation is rounded by itself: forward and backward pass (and whoever computes z by the formula) agree
-// on its sign.  Elsewhere r scale is one factor.
+// z from x - mean, for the slope.  Behind a ReLU each operation is rounded by itself: whoever computes z by the formula agrees on its sign.  Elsewhere
+// (and in the forward pass, whose output does not jump) r scale is one factor.
 template <int ACT>
 __device__ __forceinline__ float affine(float xc, float r, float scale, float slope, float shift) {
   if (ACT == SASGD_ACT_RELU) {
@@ -120,7 +126,9 @@ __device__ __forceinline__ float param(const GroupNormArgs& A, uintptr_t at, int
   return A.param_bf16 ? bf2f(((const bf16_t*)at)[c]) : ((const float*)at)[c];
 }
 
-constexpr int kLaneChannels = 64;    // channels of a group up to which one lane adds them
+// Values of a group up to which one lane adds them, a wavefront above (by lanes and by wavefronts: 5 values of each of 32 groups, 16 x 32 x 32 x 320
+// forward, 18 and 21 us; 64 of one, 256 x 4 x 4 x 512, 12 and 7; 43 of one, 30 x 23 x 20 x 43 gradient, 14 and 12).
+constexpr int kLaneChannels = 8;
 
 // Scales and shifts of the workgroup's channels, a lane a channel, to LDS: a lane has its eight from there instead of sixteen loads of its own (behind
 // the next barrier).  Fetched in front of the values and written behind them: what waits for them does not wait for the values.
@@ -256,7 +264,7 @@ __device__ __forceinline__ void unit_moments(const float (&sum)[U], const float 
 }
 
 // The workgroup's groups from the moments of their `cpg` units (mean[c], m2[c] of `np` values each): done(g, mean, sum of squared distances).  A lane a
-// group, or a wavefront a group where they have many channels (320 channels in 32 groups by wavefronts: 4 us of a workgroup's 9).
+// group, or a wavefront a group where they have many units.
 template <typename F>
 __device__ __forceinline__ void group_moments(const float* mean, const float* m2, int groups, int cpg, int np, F done) {
   const int t = threadIdx.x, T = blockDim.x;
@@ -476,7 +484,7 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
 }
 
 // Images that no workgroup can hold, first launch: the moments of a chunk of positions.  LDS: rows [2 threads U], red [threads], mean and m2 of the units
-constexpr int kAhead = 8;            // loads of a lane on their way
+constexpr int kAhead = 8;            // loads of a lane on their way (288 x 54 x 54 x 96 forward with 4, 8, 16: 98, 94, 102 us)
 template <typename T, int V, int U>
 __global__ __launch_bounds__(256) void group_norm_chunk_kernel(const GroupNormArgs A) {
   extern __shared__ float lds[];
@@ -958,7 +966,8 @@ __global__ __launch_bounds__(256) void group_norm_gradient_apply_kernel(const Gr
 }
 
 // dscale, dshift: rows of channel sums [rows][C][2] added, 32 channels a workgroup and 32 rows at a time.  Many rows in two launches: the first
-// leaves a row per blockIdx.y (`per` rows each).  256 rows 3 us, 2 304 in two launches 9; in one 28.
+// leaves a row per blockIdx.y (`per` rows each).  In one launch and in two, the whole gradient of n x 32 x 32 x 32: n = 256 20 and 23 us, 512 28 and 29,
+// 2 304 111 and 105.
 constexpr int64_t kFinishRows = 512;
 template <bool LAST>
 __global__ __launch_bounds__(1024) void group_norm_finish_kernel(const GroupNormArgs A, int64_t from, int64_t rows, int64_t per, int64_t to) {
@@ -1006,11 +1015,15 @@ size_t lds_bytes(const GroupNormArgs& a, bool gradient) {
 constexpr int kHeldForward[] = {4, 8, 16, 24, 36}, kHeldBackward[] = {4, 8, 12, 16, 24}, kHeldNarrow[] = {8, 24};
 
 // Small images are held whole, in slabs of whole groups and whole vectors: the smallest that makes segments of 128 bytes a pixel, or 64 where no more
-// fit in, or all channels; smaller ones still where the launch would otherwise have fewer workgroups than the chip has places.
+// fit in, or all channels (288 x 27 x 27 x 256, bf16, in segments of 128 bytes, of 64, in chunks: gradient 78, 87, 111 us, forward 49, 61, 65).  Larger
+// ones where there are kPlenty workgroups all the same (7 x 7 x 512, with and without: 4 096 images forward 73 and 102 us, gradient 119 and 213; 512 images
+// 11 and 17, 27 and 36; with 2 048 for kPlenty 512 images stay without), smaller ones where the launch would have fewer workgroups than the chip has places.
+// Workgroups that share lines go through the caches, and hold up to eight vectors a lane (20 x 20 x 320, held and in chunks: 64 images forward 12 and
+// 21 us, 1 024 152 and 140; gradient 21 and 40, 199 and 251.  288 x 54 x 54 x 96, 36 vectors: 106 and 94).
 constexpr int64_t kPlenty = 1024;
-// Bytes of x up to which workgroups share lines, which then go through the caches (lanes hold up to eight vectors): the other way is two launches
-// and, backward, those of the chunks' sums.
-constexpr int64_t kSharedForward = 8 << 20, kSharedGradient = 32 << 20;
+// Chunks (64 x 64 x 128 in rounds of 512 and 1 024 workgroups: 16 images forward 18 and 21 us, gradient 30 and 38, 32 images 23 and 25, 42 and 49;
+// 288 x 54 x 54 x 96 forward 96 and 93.  128 x 128 x 320 in at most 64, 128 and 256: one image forward 50, 44, 56, gradient 75, 76, 90, 16 forward 90, 96, 100).
+constexpr int64_t kRound = 512, kMostChunks = 64;
 
 GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient, bool silu, int learners) {
   GroupNormPlan p;
@@ -1048,19 +1061,13 @@ GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient,
       if (fits(256, held)) return true;
     return false;
   };
-    const int64_t all = s.images * learners * s.positions * s.channels * size;
   auto slabs = [&](int slab) { return s.images * learners * ((s.channels + slab - 1) / slab); };
   auto shares_lines = [&](int slab) { return slab < s.channels && ((slab * size) % 64 != 0 || (s.channels * size) % 64 != 0); };
   for (int bytes = 128; bytes >= 64; bytes /= 2) {
     int slab = std::min(s.channels, (bytes / size + unit - 1) / unit * unit);
     // many small images: larger slabs while there are workgroups enough and a lane holds no more than eight vectors
     while (slab < s.channels && slabs(slab * 2) >= kPlenty && (int64_t)std::min(slab * 2, s.channels) / p.vec * s.positions <= 256 * 8) slab = std::min(slab * 2, s.channels);
-    while (slab > unit && slabs(slab) < 512) {
-      const int less = std::max(unit, slab / 2 / unit * unit);
-      if (shares_lines(less) && all > (gradient ? kSharedGradient : kSharedForward)) break;
-      slab = less;
-    }
-    if (shares_lines(slab) && all > (gradient ? kSharedGradient : kSharedForward)) continue;
+    while (slab > unit && slabs(slab) < 512) slab = std::max(unit, slab / 2 / unit * unit);
     if (!take(slab)) continue;
     p.once = !shares_lines(slab);
     if (p.once || p.held <= 8) return p;
@@ -1070,10 +1077,10 @@ GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient,
   p.slabs = 1;
   p.threads = 256;
   p.held = 0;
-  // chunks of 64 KiB, smaller ones where that makes fewer than 1 024 workgroups, at most 64 an image and at least 16 KiB
+  // chunks of about 64 KiB, and whole rounds of kRound workgroups of them
   const int64_t image = (int64_t)s.positions * s.channels * size, images = std::max<int64_t>(1, s.images * learners);
-  int64_t chunks = std::max((image + 65535) / 65536, (1024 + images - 1) / images);
-  chunks = std::min(std::min(chunks, image / 16384), (int64_t)64);
+  const int64_t rounds = (images * image + kRound * 65536 - 1) / (kRound * 65536);
+  int64_t chunks = std::min(std::min(kRound * rounds / images, image / 16384), kMostChunks);
   chunks = std::max<int64_t>(1, chunks);
   p.chunk = (int)((s.positions + chunks - 1) / chunks);
   p.chunks = (s.positions + p.chunk - 1) / p.chunk;

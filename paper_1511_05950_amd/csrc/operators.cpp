@@ -64,6 +64,7 @@ const char* group_norm_args(const sasgd_norm_shape* shape, const void* x, const 
   a.y_image = shape->y_image ? shape->y_image : a.y_pixel * shape->positions;
   if (a.x_pixel > ((int64_t)1 << 32) || a.y_pixel > ((int64_t)1 << 32) || a.x_image > ((int64_t)1 << 40) || a.y_image > ((int64_t)1 << 40)) return "stride out of range";
   if (a.s.images > ((int64_t)1 << 31)) return "too many images for a launch";
+  if (shape->images > 1 && a.y_image < (shape->positions - 1) * a.y_pixel + shape->channels) return "images that are written overlap";
   if (shape->images > 0 && (!x || !y)) return "null tensor";
   const uintptr_t low = (uintptr_t)x | (uintptr_t)y | (uintptr_t)dx;
   if (low & (size - 1)) return "tensors must be aligned to their elements";

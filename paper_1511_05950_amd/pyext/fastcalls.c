@@ -559,6 +559,8 @@ static int pixels(const char* name, const view* v, int64_t* positions, int64_t* 
     *positions *= v->shape[k];
   }
   *image = v->shape[0] > 1 ? v->stride[0] : *pixel * *positions;
+  /* (a stride of 0 would stand for a dense tensor) */
+  if ((*positions > 1 && *pixel < v->shape[last]) || (v->shape[0] > 1 && *image == 0)) return bad(PyExc_ValueError, name, "must not have its values in one place");
   return 0;
 }
 static int same_shape(const view* a, const view* b) {

@@ -297,3 +297,11 @@ def test_what_the_binding_refuses():
         binding.groupNormGradient(x, w, w, 2, st, y, x.new_zeros(2, 4, 4, 16)[..., :8], workspace=torch.zeros(4096, device="cuda"))
     with pytest.raises(binding.SasgdError):
         binding.groupNormGradient(x, w, w, 2, st, y, x)             # no workspace
+    # expanded tensors: values in one place
+    for bad in (x[:1].expand(2, 4, 4, 8), x[:, :1, :1].expand(2, 4, 4, 8)):
+        with pytest.raises(ValueError):
+            binding.groupNorm(bad, w, w, 2, y, st)
+        with pytest.raises(ValueError):
+            binding.groupNormGradient(x, w, w, 2, st, bad, y, workspace=torch.zeros(4096, device="cuda"))
+    with pytest.raises(ValueError):
+        binding.groupNorm(x, w[:1].expand(8), w, 2, y, st)

@@ -25,7 +25,7 @@ BOTH = [
     (dict(no_shape=1), "shape"), (dict(images=-1), "images"), (dict(positions=0), "positions"), (dict(positions=(1 << 26) + 1), "positions"),
     (dict(channels=0), "channels"), (dict(channels=4100), "channels"), (dict(groups=0), "groups"), (dict(groups=5), "groups"), (dict(groups=64), "groups"),
     (dict(type=2), "type"), (dict(ptype=-1), "type"), (dict(act=3), "activation"), (dict(eps=0.0), "eps"), (dict(eps=float("nan")), "eps"),
-    (dict(eps=float("inf")), "eps"), (dict(xp=31), "overlap"), (dict(yp=31), "overlap"), (dict(xi=-1), "stride"), (dict(yi=1 << 41), "stride"),
+    (dict(eps=float("inf")), "eps"), (dict(xp=31), "overlap"), (dict(yp=31), "overlap"), (dict(xi=-1), "stride"), (dict(yi=31), "overlap"), (dict(yi=2047), "overlap"), (dict(yi=1 << 41), "stride"),
     (dict(x=None), "null"), (dict(y=None), "null"), (dict(x=A + 2), "aligned"), (dict(y=A + 2), "aligned"), (dict(scale=A + 2), "scale"),
     (dict(stats=A + 4), "stats"), (dict(channels=2048, groups=1, x=A + 4), "1024"), (dict(channels=1026, groups=1), "1024"),
     (dict(images=1 << 40), "too many images"),
