@@ -283,12 +283,12 @@ int sasgd_useAdamW(sasgd_ctx* ctx, const sasgd_adamw* rule, const sasgd_moments*
  * for streams, errors and graphs; nothing is allocated).  For every image and every group of channels / groups consecutive channels, over
  * the m = positions channels / groups values:
  *     mean = sum x / m;   r = 1 / sqrt(sum (x - mean)^2 / m + eps);   z = (x - mean) r scale + shift;   y = act(z)
- * Value c of position p of image n lies at x + n x_image + p x_pixel + c (elements; dx like x), and likewise for y (dy like y); a stride
+ * Value c of position p of image n lies at x + n x_image + p x_pixel + c (elements), and likewise for y (dy and dx like y); a stride
  * of 0 stands for a dense tensor.  Pointers need the alignment of their elements; where channels, strides and pointers are whole 16 bytes,
  * 16 are moved at a time. */
 enum { SASGD_ACT_NONE = 0, SASGD_ACT_RELU = 1, SASGD_ACT_SILU = 2 };   /* silu(z) = z / (1 + exp(-z)); relu'(0) = 0 */
 typedef struct {
-  int64_t images;           /* >= 0                                                                       */
+  int64_t images;           /* 0 .. 2^31                                                                  */
   int64_t positions;        /* height x width, 1 .. 2^26                                                  */
   int32_t channels, groups; /* groups divides channels; at most 4096 channels, or 1024 where they are not moved 16 bytes at a time */
   int32_t type;             /* SASGD_FP32 or SASGD_BF16: of x, y, dy, dx; sums and statistics are fp32    */
@@ -302,7 +302,9 @@ typedef struct {
 int sasgd_groupNormWorkspace(const sasgd_norm_shape* shape, int32_t gradient, size_t* out_bytes);
 
 /* groupNorm.  scale, shift: device [channels], or NULL for ones and zeros.  stats_dev: optional device float32 [images][groups][2], receives
- * mean and r, which the backward pass needs.  y_dev may be x_dev (with x's strides); else what is written lies apart from what is read, here and below.  workspace_dev: 16-byte aligned, any contents.
+ * mean and r, which the backward pass needs.  y_dev may be x_dev (with x's strides); else what is written lies apart from what is read,
+ * here and below.  Images of y may lie in each other's gaps (positions first), and overlap nowhere.  workspace_dev: 16-byte aligned, any
+ * contents.
  * Errors: EINVAL (argument), EHIP. */
 int sasgd_groupNorm(const sasgd_norm_shape* shape, const void* x_dev, const void* scale_dev, const void* shift_dev, void* y_dev, float* stats_dev,
                     void* workspace_dev, size_t workspace_bytes, void* stream, char* err, size_t err_len);
@@ -311,8 +313,7 @@ int sasgd_groupNorm(const sasgd_norm_shape* shape, const void* x_dev, const void
  *     dshift = sum dz;   dscale = sum dz xhat   over images and positions, in a fixed order;
  *     dx = r (scale dz - (sum scale dz + xhat sum scale dz xhat) / m)   the sums over the group
  * z is computed again: (x - mean) r, times scale, plus shift, each rounded (where |z| is a rounding or two the forward pass may have seen its
- * other sign).  dx_dev, dscale_dev, dshift_dev (float32 [channels]): each optional; dx_dev may
- * be dy_dev.  No images: dscale and dshift become 0.  Errors: EINVAL (argument), EHIP. */
+ * other sign).  dx_dev, dscale_dev, dshift_dev (float32 [channels]): each optional; dx_dev may be dy_dev.  No images: dscale and dshift become 0.  Errors: EINVAL (argument), EHIP. */
 int sasgd_groupNormGradient(const sasgd_norm_shape* shape, const void* x_dev, const void* scale_dev, const void* shift_dev, const float* stats_dev,
                             const void* dy_dev, void* dx_dev, float* dscale_dev, float* dshift_dev, void* workspace_dev, size_t workspace_bytes,
                             void* stream, char* err, size_t err_len);

@@ -587,7 +587,7 @@ __global__ __launch_bounds__(256) void group_norm_apply_kernel(const GroupNormAr
     return make_float2(n * d, n * cpg * d * d + p.y);
   });
   for (int g = t; g < G; g += threads) {
-    const float s = group[2 * g] / total, m2 = fmaxf(group[2 * g + 1] - total * cpg * s * s, 0.f);
+    const float s = group[2 * g] / total, m2 = __builtin_elementwise_maximum(group[2 * g + 1] - total * cpg * s * s, 0.f);       // (NaN stays)
     const float mu = parts[g].x + s, r = 1.f / sqrtf(m2 / (total * cpg) + A.eps);
     group[2 * g] = mu;
     group[2 * g + 1] = r;
@@ -1079,7 +1079,7 @@ GroupNormPlan group_norm_plan(const GroupNormShape& s, bool wide, bool gradient,
   p.held = 0;
   // chunks of about 64 KiB, and whole rounds of kRound workgroups of them
   const int64_t image = (int64_t)s.positions * s.channels * size, images = std::max<int64_t>(1, s.images * learners);
-  const int64_t rounds = (images * image + kRound * 65536 - 1) / (kRound * 65536);
+  const int64_t rounds = (images * ((image + 1023) / 1024) + kRound * 64 - 1) / (kRound * 64);
   int64_t chunks = std::min(std::min(kRound * rounds / images, image / 16384), kMostChunks);
   chunks = std::max<int64_t>(1, chunks);
   p.chunk = (int)((s.positions + chunks - 1) / chunks);

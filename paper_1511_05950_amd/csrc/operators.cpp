@@ -36,6 +36,7 @@ constexpr int64_t kMostElements = (int64_t)1 << 34;     // of a tensor and of a 
 const char* shape_error(const sasgd_norm_shape* s) {
   if (!s) return "null shape";
   if (s->images < 0 || s->positions < 1 || s->positions > kNormPositions) return "images or positions out of range";
+  if (s->images > ((int64_t)1 << 31)) return "too many images for a launch";
   if (s->channels < 1 || s->channels > kWideNormChannels || s->groups < 1 || s->channels % s->groups != 0) return "channels must be 1..4096 and a multiple of groups";
   if ((s->type != SASGD_FP32 && s->type != SASGD_BF16) || (s->param_type != SASGD_FP32 && s->param_type != SASGD_BF16)) return "unknown type";
   if (s->activation < SASGD_ACT_NONE || s->activation > SASGD_ACT_SILU) return "unknown activation";
@@ -63,9 +64,12 @@ const char* group_norm_args(const sasgd_norm_shape* shape, const void* x, const 
   a.x_image = shape->x_image ? shape->x_image : a.x_pixel * shape->positions;
   a.y_image = shape->y_image ? shape->y_image : a.y_pixel * shape->positions;
   if (a.x_pixel > ((int64_t)1 << 32) || a.y_pixel > ((int64_t)1 << 32) || a.x_image > ((int64_t)1 << 40) || a.y_image > ((int64_t)1 << 40)) return "stride out of range";
-  if (a.s.images > ((int64_t)1 << 31)) return "too many images for a launch";
-  if (shape->images > 1 && a.y_image < (shape->positions - 1) * a.y_pixel + shape->channels) return "images that are written overlap";
+  // images one behind the other, or (positions first) side by side in every position
+  if (shape->images > 1 && a.y_image < (shape->positions - 1) * a.y_pixel + shape->channels &&
+      (a.y_image < shape->channels || (shape->positions > 1 && a.y_pixel < (shape->images - 1) * a.y_image + shape->channels)))
+    return "images that are written overlap";
   if (shape->images > 0 && (!x || !y)) return "null tensor";
+  if (!gradient && x == y && (a.x_pixel != a.y_pixel || a.x_image != a.y_image)) return "in place x and y need the same strides";
   const uintptr_t low = (uintptr_t)x | (uintptr_t)y | (uintptr_t)dx;
   if (low & (size - 1)) return "tensors must be aligned to their elements";
   const int psize = shape->param_type == SASGD_BF16 ? 2 : 4;

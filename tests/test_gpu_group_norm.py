@@ -162,6 +162,52 @@ def test_strides_and_alignment(dims, kind, xpad, ypad, shift):
     c.outside()
 
 
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dims", [
+    (40, 20, 20, 320, 32), (70, 7, 7, 480, 32), (1100, 7, 7, 64, 4),          # workgroups that share lines; larger slabs of many small images
+    (2, 48, 50, 256, 256), (1, 48, 50, 4096, 4096), (1, 10, 260, 4096, 1),    # as many groups as channels, and one of all, in chunks
+    (2, 70, 71, 24, 8), (1, 300, 200, 8, 8), (3, 90, 91, 1, 1), (2, 2, 5000, 6, 2),
+    (17, 64, 65, 128, 8), (530, 1, 2, 40, 5)])
+def test_how_calls_are_cut(dims, kind):
+    c = Case(*dims, kind, "silu" if dims[0] % 2 else "relu", seed=sum(dims) + 1)
+    c.run()
+    c.check()
+    c.outside()
+
+
+@pytest.mark.parametrize("dims", [(5, 10, 12, 32, 4), (2, 61, 50, 48, 3), (3, 9, 7, 43, 1)])
+def test_positions_first(dims):
+    """Images side by side in every position: as with dense images."""
+    from paper_1511_05950_amd import binding
+    a, b = (Case(*dims, torch.bfloat16, "silu", seed=9) for _ in range(2))
+    for name in ("x", "y", "dy", "dx"):
+        t = getattr(b, name)
+        to = t.new_empty(t.shape[1], t.shape[2], t.shape[0], t.shape[3]).permute(2, 0, 1, 3)
+        to.copy_(t)
+        setattr(b, name, to)
+    a.run()
+    b.run()
+    for name in ("y", "stats", "dx", "dscale", "dshift"):
+        assert torch.equal(getattr(a, name), getattr(b, name)), name
+    with pytest.raises(binding.SasgdError):           # images of y that overlap
+        binding.groupNorm(a.x, None, None, dims[4], a.y.as_strided(a.y.shape, (1,) + a.y.stride()[1:]), workspace=a.work(False))
+
+
+def test_offsets_beyond_32_bits():
+    """Images 2^32 + 64 elements apart."""
+    a, b = (Case(2, 30, 31, 32, 4, torch.bfloat16, "relu", seed=5) for _ in range(2))
+    for name in ("x", "y", "dy", "dx"):
+        t = getattr(b, name)
+        apart = (1 << 32) + 64
+        to = t.new_empty(apart + t[0].numel()).as_strided(t.shape, (apart,) + t.stride()[1:])
+        to.copy_(t)
+        setattr(b, name, to)
+    a.run()
+    b.run()
+    for name in ("y", "stats", "dx", "dscale", "dshift"):
+        assert torch.equal(getattr(a, name), getattr(b, name)), name
+
+
 @pytest.mark.parametrize("params", [None, "fp32", "bf16"])
 def test_types_of_parameters(params):
     c = Case(3, 11, 8, 40, 5, torch.bfloat16, "none", params=params)
@@ -206,6 +252,19 @@ def test_what_is_not_finite_stays_in_its_group(bad):
     hit = np.zeros((2, 8, 8, 16), bool)
     hit[1, :, :, 4:8] = True
     assert np.array_equal(np.isnan(f64(c.y)), hit) and np.all(np.isfinite(f64(c.dx)[~hit]))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+def test_what_is_not_finite_stays_in_its_group_in_chunks(bad, kind):
+    c = Case(2, 61, 50, 48, 3, kind, "silu")
+    c.x[1, 33, 3, 20] = bad
+    c.run()
+    hit = np.zeros((2, 61, 50, 48), bool)
+    hit[1, :, :, 16:32] = True
+    assert np.array_equal(np.isnan(f64(c.y)), hit) and np.all(np.isfinite(f64(c.dx)[~hit])) and np.all(np.isnan(f64(c.dx)[hit]))
+    st = f64(c.stats)
+    assert np.all(np.isnan(st[1, 1, 1])) and np.all(np.isfinite(np.delete(st.reshape(6, 2), 4, 0)))
 
 
 @pytest.mark.parametrize("which", ["dx", "dscale", "dshift"])

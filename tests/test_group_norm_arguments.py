@@ -28,7 +28,7 @@ BOTH = [
     (dict(eps=float("inf")), "eps"), (dict(xp=31), "overlap"), (dict(yp=31), "overlap"), (dict(xi=-1), "stride"), (dict(yi=31), "overlap"), (dict(yi=2047), "overlap"), (dict(yi=1 << 41), "stride"),
     (dict(x=None), "null"), (dict(y=None), "null"), (dict(x=A + 2), "aligned"), (dict(y=A + 2), "aligned"), (dict(scale=A + 2), "scale"),
     (dict(stats=A + 4), "stats"), (dict(channels=2048, groups=1, x=A + 4), "1024"), (dict(channels=1026, groups=1), "1024"),
-    (dict(images=1 << 40), "too many images"),
+    (dict(images=1 << 40), "too many images"), (dict(yi=32, yp=127), "overlap"), (dict(yi=31, yp=1 << 20), "overlap"),
     (dict(positions=1 << 20, work=None), "workspace"), (dict(positions=1 << 20, work=A + 8), "workspace"), (dict(positions=1 << 20, bytes=15), "workspace"),
 ]
 
@@ -46,6 +46,12 @@ def test_gradient_refused(kw, word):
     assert rc == b.EINVAL and word in msg
 
 
+@pytest.mark.parametrize("kw", [dict(yp=40), dict(xp=40), dict(yi=4096), dict(xi=32, xp=128)])
+def test_in_place_with_other_strides_is_refused(kw):
+    rc, msg = call(False, x=A, y=A, **kw)
+    assert rc == b.EINVAL and "same strides" in msg
+
+
 def test_no_images_is_no_error():
     assert call(False, images=0, x=None, y=None, stats=None, work=None)[0] == b.OK
     assert call(True, images=0, x=None, y=None, stats=None, dx=None, ds=None, work=None)[0] == b.OK
@@ -57,5 +63,10 @@ def test_workspace():
     assert b.load().sasgd_groupNormWorkspace(ctypes.byref(s), 0, ctypes.byref(out)) == b.OK and out.value == 0
     assert b.load().sasgd_groupNormWorkspace(ctypes.byref(s), 1, ctypes.byref(out)) == b.OK and out.value >= 4 * 32 * 8
     assert b.load().sasgd_groupNormWorkspace(ctypes.byref(s), 0, None) == b.EINVAL
+    # the largest shape does not overflow; one image more is refused
+    big = b.SasgdNormShape(1 << 31, 1 << 26, 4096, 1, 0, 0, 0, 1e-5, 0, 0, 0, 0)
+    assert b.load().sasgd_groupNormWorkspace(ctypes.byref(big), 1, ctypes.byref(out)) == b.OK and out.value >= (1 << 31) * 4096 * 8
+    big.images += 1
+    assert b.load().sasgd_groupNormWorkspace(ctypes.byref(big), 1, ctypes.byref(out)) == b.EINVAL
     s.groups = 3
     assert b.load().sasgd_groupNormWorkspace(ctypes.byref(s), 0, ctypes.byref(out)) == b.EINVAL
