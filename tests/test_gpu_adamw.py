@@ -244,6 +244,29 @@ def test_gradients_that_are_flat_vectors(c, states):
     assert torch.equal(a.flat, b.flat) and torch.equal(a.m.view(torch.uint8), b.m.view(torch.uint8)) and torch.equal(a.v.view(torch.uint8), b.v.view(torch.uint8))
 
 
+@pytest.mark.parametrize("states", ["fp32", "e4m3"])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_flat_vectors_of_bf16_in_the_longest_window(pad, states):
+    """64 flat bf16 vectors, the last the first once more, with copies and weights that go elsewhere."""
+    a, b = (Run([1025, 0, 64, 300] * 30, torch.bfloat16, states, 64, "constant", outs=True, seed=6) for _ in range(2))
+    a.lists[63] = a.lists[0]
+    buffers = []
+    for l in range(63):
+        flat, at, lists = torch.zeros(sum(b.sizes) + 64, device="cuda", dtype=torch.bfloat16), pad, []
+        for n, g in zip(b.sizes, b.lists[l]):
+            flat[at:at + n] = g
+            lists.append(flat[at:at + n])
+            at += n
+        b.lists[l] = lists
+        buffers.append(flat)
+    b.lists[63] = b.lists[0]
+    for t in (1, 2):
+        a.step(t)
+        b.step(t)
+    for x, y in ((a.out_flat, b.out_flat), (a.copy_flat, b.copy_flat), (a.m.view(torch.uint8), b.m.view(torch.uint8)), (a.v.view(torch.uint8), b.v.view(torch.uint8))):
+        assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("kw", [dict(beta1=0.0), dict(beta2=0.0), dict(beta1=0.0, beta2=0.0, eps=1.0), dict(wd=0.0, alpha0=0.0), dict(std=1e-12), dict(std=1e8)])
 @pytest.mark.parametrize("states", ["fp32", "e4m3"])
 def test_extreme_rules_and_gradients(states, kw):
