@@ -11,8 +11,9 @@
 // Sums go by units of neighbouring channels (one, two, or a lane's whole vector where a group is whole vectors; one in the backward pass, whose dscale
 // and dshift want them): a lane owns 16 bytes of channels at a fixed place of the pixel and walks positions, the rows of lanes are added through LDS in a
 // fixed order, and groups are put together from their units, whatever number of channels a group has.  Variances are sums of squared distances
-// from the mean of what is summed, joined by sum of those + sum of count x (mean - joint mean)^2, from lanes to units to groups: no difference of
-// large sums.
+// from the mean of what is summed, joined by sum of those + sum of count x (mean - joint mean)^2, from lanes to units to groups.  Two differences of sums are
+// left: a lane's squares less its sum's (Moments, DotMoments), good to 32 bits or to 256 roundings of them, and that of an image's at most 64 chunks
+// (group_norm_apply_kernel), of distances from the first one's mean, good to 64 times the few roundings of its sums.
 //
 // What bounds it now (MI355X; a copy of these tensors runs at 4.7 TB/s): bf16 2 304 x 32 x 32 x 32 gradient 105 us, 4.3 TB/s; 288 x 27 x 27 x 256
 // gradient 78 us, 4.1 TB/s: HBM, and the vector ALU between the phases of a workgroup.  288 x 54 x 54 x 96 forward 96 us: 35 of statistics, 59 at the copy's
@@ -295,56 +296,96 @@ __device__ __forceinline__ void group_moments(const float* mean, const float* m2
   }
 }
 
-// What a lane adds up of its positions.  Distances from the lane's first value: the cancellation costs at most as many roundings of the
-// result as there are values, as none is further from their mean than the root of that many variances.
+// What a lane adds up of its positions, by units: start, add, (now and then) fold, close.  close gives sum and squared distances of the lane's mean of `count`
+// positions; false: the squared distances are to be added up again from that mean.
+//
+// Where the values are not kept: sums and squares in 64 bits, of distances from the lane's first value.  A square of two fp32 numbers is exact there, so
+// however many values a lane has and however far the first one is from the rest, what is left of the difference is good to 32 bits: the first value is one of
+// them, so its square is at most the sum of squared distances, and the difference cancels by a factor of their number at most, below 2^29.
 template <typename T, int V, int U>
 struct Moments {
-  float first[V], s[V], q[V];
+  float first[U];
+  double s[U], q[U];
   __device__ __forceinline__ void start(const typename Raw<T, V>::type& raw, bool any) {
+    float f[V];
 #pragma unroll
-    for (int j = 0; j < V; j++) first[j] = s[j] = q[j] = 0.f;
-    if (any) unpack(raw, first);
-    if (U < V)
+    for (int k = 0; k < U; k++) {
+      first[k] = 0.f;
+      s[k] = q[k] = 0.0;
+    }
+    if (!any) return;
+    unpack(raw, f);
 #pragma unroll
-      for (int j = 0; j < V; j++) first[j] = first[j / (V / U) * (V / U)];
-    if (U < V && any) add(raw);
+    for (int k = 0; k < U; k++) first[k] = f[k * (V / U)];
+    if (U < V) add(raw);
   }
   __device__ __forceinline__ void add(const typename Raw<T, V>::type& raw) {
     float f[V];
     unpack(raw, f);
 #pragma unroll
     for (int j = 0; j < V; j++) {
-      const float e = f[j] - first[j];
-      s[j] += e;
-      q[j] = fmaf(e, e, q[j]);
+      const int k = j / (V / U);
+      // (bf16 values 2^16 apart or less: exact in 32 bits)
+      const double e = sizeof(T) == 2 ? (double)(f[j] - first[k]) : (double)f[j] - (double)first[k];
+      s[k] += e;
+      q[k] = fma(e, e, q[k]);
     }
   }
-  // sum and squared distances of the lane's mean, by units, of `count` positions; false: not to the precision wanted
-  __device__ __forceinline__ bool close(int count, float (&sum)[U], float (&dev)[U]) const {
-    constexpr int kEach = V / U;
-    const float n = (float)(count * kEach), inv = count > 0 ? 1.f / n : 0.f;
+  __device__ __forceinline__ void fold() {}
+  __device__ __forceinline__ bool close(int count, float (&sum)[U], float (&dev)[U]) {
+    const double n = (double)count * (V / U), inv = count > 0 ? 1.0 / n : 0.0;
 #pragma unroll
     for (int k = 0; k < U; k++) {
-      float a = 0.f, b = 0.f;
-#pragma unroll
-      for (int j = k * kEach; j < (k + 1) * kEach; j++) {
-        a += s[j];
-        b += q[j];
-      }
-      dev[k] = fmaxf(b - a * a * inv, 0.f);
-      sum[k] = count > 0 ? fmaf(first[k * kEach], n, a) : 0.f;
+      dev[k] = (float)fmax(q[k] - s[k] * s[k] * inv, 0.0);
+      sum[k] = count > 0 ? (float)fma((double)first[k], n, s[k]) : 0.f;
     }
     return true;
   }
 };
+// Where they are, in registers: sums in 32 bits (at most 144 values), then the distances in a second pass (the 64-bit operations take longer: 30 x 23 x 20 x 43
+// fp32 9.2 us with them, 8.4 so).
+template <typename T, int V, int U>
+struct HeldMoments {
+  float first[U], s[U];
+  __device__ __forceinline__ void start(const typename Raw<T, V>::type& raw, bool any) {
+    float f[V];
+#pragma unroll
+    for (int k = 0; k < U; k++) first[k] = s[k] = 0.f;
+    if (!any) return;
+    unpack(raw, f);
+#pragma unroll
+    for (int k = 0; k < U; k++) first[k] = f[k * (V / U)];
+    if (U < V) add(raw);
+  }
+  __device__ __forceinline__ void add(const typename Raw<T, V>::type& raw) {
+    float f[V];
+    unpack(raw, f);
+#pragma unroll
+    for (int j = 0; j < V; j++) s[j / (V / U)] += f[j] - first[j / (V / U)];
+  }
+  __device__ __forceinline__ bool close(int count, float (&sum)[U], float (&dev)[U]) {
+    const float n = (float)(count * (V / U));
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      dev[k] = 0.f;
+      sum[k] = count > 0 ? fmaf(first[k], n, s[k]) : 0.f;
+    }
+    return false;
+  }
+};
 // bf16 in units of two channels and more: pairs by the dot product instructions, one instruction a value instead of four.  Distances from 0, so
-// where a lane's values are far from 0 against their spread its squared distances are added up again from its mean.
+// where a lane's values are far from 0 against their spread its squared distances are added up again from its mean.  Sums of kFold vectors in
+// 32 bits, then in 64: a lane's squares are off by less than kFold roundings, and what is left of them after the check by eight times that.
+constexpr int kFold = 32;
 template <int U>
 struct DotMoments {
   float s[4], q[4];
+  double sum_[U], squares_[U];
   __device__ __forceinline__ void start(const uint4& raw, bool any) {
 #pragma unroll
     for (int j = 0; j < 4; j++) s[j] = q[j] = 0.f;
+#pragma unroll
+    for (int k = 0; k < U; k++) sum_[k] = squares_[k] = 0.0;
     if (any) add(raw);
   }
   __device__ __forceinline__ void add(const uint4& raw) {
@@ -358,26 +399,29 @@ struct DotMoments {
       q[k] = __builtin_amdgcn_fdot2_f32_bf16(x, x, q[k], false);
     }
   }
-  __device__ __forceinline__ bool close(int count, float (&sum)[U], float (&dev)[U]) const {
-    constexpr int kEach = 4 / U;
-    const float inv = count > 0 ? 1.f / (float)(count * 8 / U) : 0.f;
+  __device__ __forceinline__ void fold() {
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      sum_[j / (4 / U)] += s[j];
+      squares_[j / (4 / U)] += q[j];
+      s[j] = q[j] = 0.f;
+    }
+  }
+  __device__ __forceinline__ bool close(int count, float (&sum)[U], float (&dev)[U]) {
+    const double inv = count > 0 ? 1.0 / (double)((int64_t)count * (8 / U)) : 0.0;
     bool fine = true;
+    fold();
 #pragma unroll
     for (int k = 0; k < U; k++) {
-      float a = 0.f, b = 0.f;
-#pragma unroll
-      for (int j = k * kEach; j < (k + 1) * kEach; j++) {
-        a += s[j];
-        b += q[j];
-      }
-      sum[k] = a;
-      dev[k] = fmaxf(b - a * a * inv, 0.f);
-      fine = fine && !(dev[k] < 0.125f * b);
+      sum[k] = (float)sum_[k];
+      dev[k] = (float)fmax(squares_[k] - sum_[k] * sum_[k] * inv, 0.0);
+      fine = fine && !(dev[k] < 0.125f * (float)squares_[k]);
     }
     return fine;
   }
 };
-template <typename T, int V, int U> using LaneMoments = std::conditional_t<(V == 8 && U < 8), DotMoments<U>, Moments<T, V, U>>;
+template <typename T, int V, int U, bool HELD> using LaneMoments =
+    std::conditional_t<(V == 8 && U < 8), DotMoments<U>, std::conditional_t<HELD, HeldMoments<T, V, U>, Moments<T, V, U>>>;
 // Squared distances from the lane's means, once more.
 template <typename T, int V, int U>
 __device__ __forceinline__ void add_distances(const typename Raw<T, V>::type& raw, const float (&mean)[U], float (&dev)[U]) {
@@ -424,7 +468,7 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
     par.put(A, scale + c, scale + S + c);
   }
   {
-    LaneMoments<T, V, U> mom;
+    LaneMoments<T, V, U, true> mom;
     float sum[U], dev[U];
     mom.start(held[0], count > 0);
 #pragma unroll
@@ -485,6 +529,7 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
 
 // Images that no workgroup can hold, first launch: the moments of a chunk of positions.  LDS: rows [2 threads U], red [threads], mean and m2 of the units
 constexpr int kAhead = 8;            // loads of a lane on their way (288 x 54 x 54 x 96 forward with 4, 8, 16: 98, 94, 102 us)
+static_assert(kFold % kAhead == 0, "sums are folded between loads");
 template <typename T, int V, int U>
 __global__ __launch_bounds__(256) void group_norm_chunk_kernel(const GroupNormArgs A) {
   extern __shared__ float lds[];
@@ -505,24 +550,37 @@ __global__ __launch_bounds__(256) void group_norm_chunk_kernel(const GroupNormAr
     const int count = count_of(l, np);
     const T* x = x0 + l.row * A.x_pixel + c0 + l.col * V;
     const int64_t step = l.rows * A.x_pixel;
-    LaneMoments<T, V, U> mom;
+    LaneMoments<T, V, U, false> mom;
     float sum[U], dev[U];
     for (int k = 0; k < count || k == 0; k += kAhead) {
       raw_t in[kAhead];
       load_rows<false>(in, x + k * step, step, count - k);
       if (k == 0) mom.start(in[0], count > 0);
+      else if (k % kFold == 0) mom.fold();
 #pragma unroll
       for (int i = 0; i < kAhead; i++)
         if (k + i < count && k + i > 0) mom.add(in[i]);
     }
     if (!mom.close(count, sum, dev)) {
-      float mu[U];
+      float mu[U], part[U];
+      double total[U];
 #pragma unroll
       for (int j = 0; j < U; j++) {
         mu[j] = sum[j] / (float)(count * (V / U));
-        dev[j] = 0.f;
+        total[j] = 0.0;
+        part[j] = 0.f;
       }
-      for (int k = 0; k < count; k++) add_distances<T, V, U>(*(const raw_t*)(x + k * step), mu, dev);
+      for (int k = 0; k < count; k++) {
+        add_distances<T, V, U>(*(const raw_t*)(x + k * step), mu, part);
+        if (k % kFold == kFold - 1 || k == count - 1)
+#pragma unroll
+          for (int j = 0; j < U; j++) {
+            total[j] += part[j];
+            part[j] = 0.f;
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < U; j++) dev[j] = (float)total[j];
     }
     unit_moments<V, U>(sum, dev, cols, l, np, rows, red, mean + c0 / (V / U), m2 + c0 / (V / U));
   }
