@@ -89,6 +89,14 @@ __device__ __forceinline__ float round8(float y, uint32_t chance) {
   return fminf(r - off, 448.0f);
 }
 
+// The hardware's root, 1 ulp.  It takes denormal numbers for 0, which would leave an epsilon below their roots (1e-19) alone under the fraction: they are
+// moved up by 2^64 and back.
+__device__ __forceinline__ float root(float v) {
+  const bool small = v < 0x1p-96f;
+  const float r = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v);
+  return small ? r * 0x1p-32f : r;
+}
+
 // ------------------------------------------------------------------------------------------------ one block
 // What a wavefront holds of a block: element e of lane `lane` is 4 lane + j (vector moves) or lane + 64 j.
 template <bool VEC>
@@ -205,7 +213,7 @@ __device__ __forceinline__ void adamw_blocks(const AdamwLaunch& A, const AdamwSt
       v[r][j] = v[r][j] * A.beta2 + (gg * gg) * A.rest2;
       // What is kept is rounded operation by operation; the weight's move takes the hardware's root and reciprocal (1 ulp each): a
       // division and two roots by the book were 40 of the 130 instructions of an element with 8-bit moments.
-      u[j] = E4M3 ? sqrtf(v[r][j]) : __builtin_amdgcn_sqrtf(v[r][j]);
+      u[j] = E4M3 ? sqrtf(v[r][j]) : root(v[r][j]);
       const float move = (m[r][j] * S.pace) * __builtin_amdgcn_rcpf(u[j] * S.root + A.epsilon);
       if (!S.skip) th[r][j] = th[r][j] * A.keep - move;
       if (E4M3) {
