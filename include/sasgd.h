@@ -312,8 +312,8 @@ int sasgd_groupNorm(const sasgd_norm_shape* shape, const void* x_dev, const void
 /* groupNormGradient: with dz = dy act'(z) and xhat = (x - mean) r
  *     dshift = sum dz;   dscale = sum dz xhat   over images and positions, in a fixed order;
  *     dx = r (scale dz - (sum scale dz + xhat sum scale dz xhat) / m)   the sums over the group
- * z is computed again: (x - mean) r, times scale, plus shift, each rounded (where |z| is a rounding or two the forward pass may have seen its
- * other sign).  dx_dev, dscale_dev, dshift_dev (float32 [channels]): each optional; dx_dev may be dy_dev.  No images: dscale and dshift become 0.  Errors: EINVAL (argument), EHIP. */
+ * z is computed again, by the operations of the forward pass (behind a ReLU (x - mean) r, times scale, plus shift, each rounded): dy passes where y is
+ * positive.  dx_dev, dscale_dev, dshift_dev (float32 [channels]): each optional; dx_dev may be dy_dev.  No images: dscale and dshift become 0.  Errors: EINVAL (argument), EHIP. */
 int sasgd_groupNormGradient(const sasgd_norm_shape* shape, const void* x_dev, const void* scale_dev, const void* shift_dev, const float* stats_dev,
                             const void* dy_dev, void* dx_dev, float* dscale_dev, float* dshift_dev, void* workspace_dev, size_t workspace_bytes,
                             void* stream, char* err, size_t err_len);

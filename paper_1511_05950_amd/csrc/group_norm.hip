@@ -102,8 +102,8 @@ __device__ __forceinline__ float activate(float z) {
   if (ACT == SASGD_ACT_SILU) return z * sigmoid(z);
   return z;
 }
-// z from x - mean, for the slope.  Behind a ReLU each operation is rounded by itself: whoever computes z by the formula agrees on its sign.  Elsewhere
-// (and in the forward pass, whose output does not jump) r scale is one factor.
+// z from x - mean.  Behind a ReLU each operation is rounded by itself, in both directions: the backward pass passes dy where the forward pass gave a positive
+// output, and whoever computes z by the formula agrees on its sign.  Elsewhere r scale is one factor.
 template <int ACT>
 __device__ __forceinline__ float affine(float xc, float r, float scale, float slope, float shift) {
   if (ACT == SASGD_ACT_RELU) {
@@ -495,22 +495,23 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
   });
   __syncthreads();
   if (count == 0) return;
-  float mu[V], slope[V], sh[V];
+  float mu[V], r[V], sc[V], sh[V], slope[V];
   if (V > 1) {                                       // (S is whole vectors: 16-byte places)
 #pragma unroll
     for (int j = 0; j < V; j += 4) {
-      *(float4*)(slope + j) = *(const float4*)(scale + first_c + j);
+      *(float4*)(sc + j) = *(const float4*)(scale + first_c + j);
       *(float4*)(sh + j) = *(const float4*)(scale + S + first_c + j);
     }
   } else {
-    slope[0] = scale[first_c];
+    sc[0] = scale[first_c];
     sh[0] = scale[S + first_c];
   }
 #pragma unroll
   for (int j = 0; j < V; j++) {
     const int g = A.by_cpg(first_c + (U == 1 ? 0 : j));
     mu[j] = group[2 * g];
-    slope[j] *= group[2 * g + 1];
+    r[j] = group[2 * g + 1];
+    slope[j] = r[j] * sc[j];
   }
   T* y = (T*)(base + A.y) + at.image * A.y_image + l.row * A.y_pixel + c0 + first_c;
   const int64_t ystep = l.rows * A.y_pixel;
@@ -520,7 +521,7 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
       float f[V];
       unpack(held[k], f);
 #pragma unroll
-      for (int j = 0; j < V; j++) f[j] = activate<ACT>(fmaf(f[j] - mu[j], slope[j], sh[j]));
+      for (int j = 0; j < V; j++) f[j] = activate<ACT>(affine<ACT>(f[j] - mu[j], r[j], sc[j], slope[j], sh[j]));
       raw_t o;
       pack(o, f);
       store_row<ONCE>((raw_t*)(y + k * ystep), o);
@@ -656,13 +657,15 @@ __global__ __launch_bounds__(256) void group_norm_apply_kernel(const GroupNormAr
     const Lanes l = lanes_of(A.cols[c0 + A.cols[0].cols * V >= C], t);
     const int count = count_of(l, np), c = c0 + l.col * V;
     if (count == 0) continue;
-    float mu[V], sh[V], slope[V];
+    float mu[V], r[V], sc[V], sh[V], slope[V];
 #pragma unroll
     for (int j = 0; j < V; j++) {
       const int g = A.by_cpg(c + j);
       mu[j] = group[2 * g];
-      slope[j] = group[2 * g + 1] * (A.has_scale ? param(A, wts + A.scale, c + j) : 1.f);
+      r[j] = group[2 * g + 1];
+      sc[j] = A.has_scale ? param(A, wts + A.scale, c + j) : 1.f;
       sh[j] = A.has_shift ? param(A, wts + A.shift, c + j) : 0.f;
+      slope[j] = r[j] * sc[j];
     }
     const T* x = xp + l.row * A.x_pixel + c;
     T* y = (T*)(base + A.y) + at.image * A.y_image + (int64_t)(p0 + l.row) * A.y_pixel + c;
@@ -671,7 +674,7 @@ __global__ __launch_bounds__(256) void group_norm_apply_kernel(const GroupNormAr
       float f[V];
       unpack(in, f);
 #pragma unroll
-      for (int j = 0; j < V; j++) f[j] = activate<ACT>(fmaf(f[j] - mu[j], slope[j], sh[j]));
+      for (int j = 0; j < V; j++) f[j] = activate<ACT>(affine<ACT>(f[j] - mu[j], r[j], sc[j], slope[j], sh[j]));
       raw_t o;
       pack(o, f);
       store_once((raw_t*)(y + k * ystep), o);
