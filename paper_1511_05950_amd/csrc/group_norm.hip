@@ -1258,28 +1258,53 @@ static hipError_t backward(const GroupNormArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// A launch holds fewer than 2^32 lanes: the images, as many at a time as that takes.  launch(a): those of a.s from a.x, a.y, a.dy, a.dx, a.stats, a.parts and
+// a.sums on, which move on behind them.
+template <typename F>
+static hipError_t by_images(GroupNormArgs& a, F launch) {
+  const int64_t parts = a.plan.whole ? a.plan.slabs : a.plan.chunks, most = (((int64_t)1 << 32) - 1) / (parts * a.plan.threads) / 8 * 8;
+  const int64_t size = a.s.bf16 ? 2 : 4, all = a.s.images;
+  hipError_t e = hipSuccess;
+  for (int64_t left = all; left > 0 && e == hipSuccess;) {
+    a.s.images = std::min(left, most);
+    e = launch(a);
+    left -= a.s.images;
+    if (left == 0) break;
+    a.x += a.s.images * a.x_image * size;
+    a.y += a.s.images * a.y_image * size;
+    a.dy += a.s.images * a.y_image * size;
+    a.dx += a.s.images * a.y_image * size;
+    a.stats += a.s.images * a.s.groups * 8;
+    a.parts += a.s.images * a.plan.chunks * a.s.groups * 8;
+    a.sums += a.s.images * a.plan.chunks * a.s.channels * 8;
+  }
+  a.s.images = all;
+  return e;
+}
+
 hipError_t launch_group_norm(GroupNormArgs& a, hipStream_t stream) {
-  if (a.s.images == 0) return hipSuccess;
   const int cpg = a.s.channels / a.s.groups;
-  if (a.s.bf16 && a.plan.vec == 8) return cpg % 8 == 0 ? forward<bf16_t, 8, 1>(a, stream) : cpg % 2 == 0 ? forward<bf16_t, 8, 4>(a, stream) : forward<bf16_t, 8, 8>(a, stream);
-  if (a.s.bf16) return forward<bf16_t, 1, 1>(a, stream);
-  if (a.plan.vec == 4) return cpg % 4 == 0 ? forward<float, 4, 1>(a, stream) : forward<float, 4, 4>(a, stream);
-  return forward<float, 1, 1>(a, stream);
+  return by_images(a, [&](GroupNormArgs& a) {
+    if (a.s.bf16 && a.plan.vec == 8) return cpg % 8 == 0 ? forward<bf16_t, 8, 1>(a, stream) : cpg % 2 == 0 ? forward<bf16_t, 8, 4>(a, stream) : forward<bf16_t, 8, 8>(a, stream);
+    if (a.s.bf16) return forward<bf16_t, 1, 1>(a, stream);
+    if (a.plan.vec == 4) return cpg % 4 == 0 ? forward<float, 4, 1>(a, stream) : forward<float, 4, 4>(a, stream);
+    return forward<float, 1, 1>(a, stream);
+  });
 }
 
 hipError_t launch_group_norm_gradient(GroupNormArgs& a, hipStream_t stream) {
-  hipError_t e = hipSuccess;
-  if (a.s.images > 0) {
+  int64_t from = a.sums;
+  hipError_t e = by_images(a, [&](GroupNormArgs& a) {
     set_columns(a, a.plan.vec);
-    if (a.s.bf16) e = a.plan.vec == 8 ? backward<bf16_t, 8>(a, stream) : backward<bf16_t, 1>(a, stream);
-    else e = a.plan.vec == 4 ? backward<float, 4>(a, stream) : backward<float, 1>(a, stream);
-  }
+    if (a.s.bf16) return a.plan.vec == 8 ? backward<bf16_t, 8>(a, stream) : backward<bf16_t, 1>(a, stream);
+    return a.plan.vec == 4 ? backward<float, 4>(a, stream) : backward<float, 1>(a, stream);
+  });
   if (e != hipSuccess || (!a.has_dscale && !a.has_dshift)) return e;
   const int64_t rows = a.s.images * a.plan.chunks, splits = finish_splits(rows);
   const uint32_t strips = (uint32_t)(a.s.channels + 31) / 32, learners = (uint32_t)a.learners;
-  int64_t from = a.sums, left = rows;
+  int64_t left = rows;
   if (splits > 0) {
-    const int64_t to = a.sums + rows * a.s.channels * 8, per = (rows + splits - 1) / splits;
+    const int64_t to = from + rows * a.s.channels * 8, per = (rows + splits - 1) / splits;
     group_norm_finish_kernel<false><<<dim3(strips, (uint32_t)splits, learners), 1024, 0, stream>>>(a, from, rows, per, to);
     e = hipGetLastError();
     if (e != hipSuccess) return e;

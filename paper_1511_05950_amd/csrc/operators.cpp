@@ -36,7 +36,7 @@ constexpr int64_t kMostElements = (int64_t)1 << 34;     // of a tensor and of a 
 const char* shape_error(const sasgd_norm_shape* s) {
   if (!s) return "null shape";
   if (s->images < 0 || s->positions < 1 || s->positions > kNormPositions) return "images or positions out of range";
-  if (s->images > ((int64_t)1 << 31)) return "too many images for a launch";
+  if (s->images > ((int64_t)1 << 31)) return "too many images";
   if (s->channels < 1 || s->channels > kWideNormChannels || s->groups < 1 || s->channels % s->groups != 0) return "channels must be 1..4096 and a multiple of groups";
   if ((s->type != SASGD_FP32 && s->type != SASGD_BF16) || (s->param_type != SASGD_FP32 && s->param_type != SASGD_BF16)) return "unknown type";
   if (s->activation < SASGD_ACT_NONE || s->activation > SASGD_ACT_SILU) return "unknown activation";
@@ -64,6 +64,8 @@ const char* group_norm_args(const sasgd_norm_shape* shape, const void* x, const 
   a.x_image = shape->x_image ? shape->x_image : a.x_pixel * shape->positions;
   a.y_image = shape->y_image ? shape->y_image : a.y_pixel * shape->positions;
   if (a.x_pixel > ((int64_t)1 << 32) || a.y_pixel > ((int64_t)1 << 32) || a.x_image > ((int64_t)1 << 40) || a.y_image > ((int64_t)1 << 40)) return "stride out of range";
+  const int64_t reach = (int64_t)1 << 48;      // (of elements: more than there are addresses)
+  if (shape->images > 1 && (a.x_image > reach / (shape->images - 1) || a.y_image > reach / (shape->images - 1))) return "stride out of range";
   // images one behind the other, or (positions first) side by side in every position
   if (shape->images > 1 && a.y_image < (shape->positions - 1) * a.y_pixel + shape->channels &&
       (a.y_image < shape->channels || (shape->positions > 1 && a.y_pixel < (shape->images - 1) * a.y_image + shape->channels)))
@@ -78,7 +80,6 @@ const char* group_norm_args(const sasgd_norm_shape* shape, const void* x, const 
   const bool wide = (low & 15) == 0 && (a.s.channels | a.x_pixel | a.y_pixel | a.x_image | a.y_image) % vec == 0;
   if (!wide && a.s.channels > kNarrowNormChannels) return "more than 1024 channels must be whole 16 bytes, in strides and pointers too";
   a.plan = group_norm_plan(a.s, wide, gradient, a.activation == SASGD_ACT_SILU, 1);
-  if ((a.s.images + 8) * (int64_t)(a.plan.whole ? a.plan.slabs : a.plan.chunks) * a.plan.threads >= ((int64_t)1 << 32)) return "too many images for a launch";
   const size_t need = group_norm_scratch_bytes(a.s, a.plan, gradient);
   if (need > 0 && (!work || ((uintptr_t)work & 15) || work_bytes < need)) return "workspace missing, too small or not 16-byte aligned";
   a.x = (int64_t)(uintptr_t)x;
