@@ -71,7 +71,7 @@ const char* group_norm_args(const sasgd_norm_shape* shape, const void* x, const 
       (a.y_image < shape->channels || (shape->positions > 1 && a.y_pixel < (shape->images - 1) * a.y_image + shape->channels)))
     return "images that are written overlap";
   if (shape->images > 0 && (!x || !y)) return "null tensor";
-  if (!gradient && x == y && (a.x_pixel != a.y_pixel || a.x_image != a.y_image)) return "in place x and y need the same strides";
+  if (!gradient && shape->images > 0 && x == y && (a.x_pixel != a.y_pixel || a.x_image != a.y_image)) return "in place x and y need the same strides";
   const uintptr_t low = (uintptr_t)x | (uintptr_t)y | (uintptr_t)dx;
   if (low & (size - 1)) return "tensors must be aligned to their elements";
   const int psize = shape->param_type == SASGD_BF16 ? 2 : 4;

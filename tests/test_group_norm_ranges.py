@@ -18,3 +18,9 @@ def test_one_image_may_lie_anywhere(gradient):
     """An image's distance to the next one is not used where there is none (the call then fails only for want of a workspace)."""
     rc, msg = call(gradient, images=1, positions=1 << 20, yi=1 << 40, xi=1 << 40, work=None)
     assert rc == b.EINVAL and "workspace" in msg, msg
+
+
+@pytest.mark.parametrize("kw", [dict(xp=40), dict(yi=4096), dict(xi=32, xp=128)])
+def test_no_images_are_not_in_place(kw):
+    """Empty tensors have no address: x and y of different strides are both at 0, which is not one tensor."""
+    assert call(False, images=0, x=None, y=None, stats=None, work=None, **kw)[0] == b.OK
