@@ -249,14 +249,17 @@ static PyObject* apply_update_no_alloc(PyObject* self, PyObject* const* a, Py_ss
     bad = address(PySequence_Fast_GET_ITEM(gs, k), &g) || (k < nst && as_integer32(PySequence_Fast_GET_ITEM(ss, k), &stale[k]));
     grads[k] = (const float*)g;
   }
-  Py_DECREF(gs);
   Py_DECREF(ss);
-  if (bad) return NULL;
-  Py_BEGIN_ALLOW_THREADS
+  if (bad) {
+    Py_DECREF(gs);
+    return NULL;
+  }
+  Py_BEGIN_ALLOW_THREADS            /* (gs may be all that holds the gradients: a generator's) */
   rc = sasgd_applyUpdateNoAlloc((const float*)tin, (float*)tout, (float*)v, (uint16_t*)shadow, P,
                                 c > SASGD_NOALLOC_MAX_GRADIENTS ? SASGD_NOALLOC_MAX_GRADIENTS + 1 : (int32_t)c, grads, stale, mode, (float)alpha0,
                                 (float)momentum, (float)decay, stream, err, sizeof(err));
   Py_END_ALLOW_THREADS
+  Py_DECREF(gs);
   if (rc) return raise_code(rc, err);
   return PyLong_FromLong(rc);
 }
@@ -432,12 +435,12 @@ static PyObject* gradient_norm(PyObject* self, PyObject* const* a, Py_ssize_t na
   failed = !grads || !numel || n > INT32_MAX;
   if (failed) PyErr_NoMemory();
   else failed = list_of(seq, n, device, &kind, grads, 1, numel, sizeof(int64_t), 0);
-  Py_DECREF(seq);
   if (!failed) {
     Py_BEGIN_ALLOW_THREADS
     rc = sasgd_gradientNorm(grads, numel, (int32_t)n, kind == KIND_OTHER ? SASGD_FP32 : kind, (float)max_norm, (float*)out.data, work, stream, err, sizeof(err));
     Py_END_ALLOW_THREADS
   }
+  Py_DECREF(seq);                     /* (it may be all that holds the gradients: a generator's) */
   PyMem_Free(grads);
   PyMem_Free(numel);
   if (failed) return NULL;
@@ -485,8 +488,8 @@ static PyObject* apply_adamw(PyObject* self, PyObject* const* a, Py_ssize_t narg
   int32_t count, device, stale[SASGD_NOALLOC_MAX_GRADIENTS];
   int kind = KIND_OTHER, rc = 0, failed = 0;
   long long step;
-  Py_ssize_t c, l;
-  PyObject *lists, *st;
+  Py_ssize_t c, l, held = 0;
+  PyObject *lists, *st, *one[SASGD_NOALLOC_MAX_GRADIENTS];      /* one[0 .. held): they may be all that holds the gradients */
   const void** grads;
   view factor;
   char err[256] = "";
@@ -517,20 +520,19 @@ static PyObject* apply_adamw(PyObject* self, PyObject* const* a, Py_ssize_t narg
     failed = 1;
   }
   for (l = 0; !failed && l < c; l++) {
-    PyObject* one = PySequence_Fast(PySequence_Fast_GET_ITEM(lists, l), "grads must be a sequence of sequences");
-    if (!one) {
+    one[l] = PySequence_Fast(PySequence_Fast_GET_ITEM(lists, l), "grads must be a sequence of sequences");
+    if (!one[l]) {
       failed = 1;
       break;
     }
-    if (PySequence_Fast_GET_SIZE(one) != count) {
+    held = l + 1;
+    if (PySequence_Fast_GET_SIZE(one[l]) != count) {
       PyErr_SetString(PyExc_ValueError, "a gradient has another number of tensors than the weights");
       failed = 1;
     } else {
-      failed = list_of(one, count, device, &kind, grads + l, (size_t)c, &((sasgd_tensor*)tensors)->numel, sizeof(sasgd_tensor), 1);
+      failed = list_of(one[l], count, device, &kind, grads + l, (size_t)c, &((sasgd_tensor*)tensors)->numel, sizeof(sasgd_tensor), 1);
     }
-    Py_DECREF(one);
   }
-  Py_DECREF(lists);
   if (!failed) {
     if (kind != KIND_OTHER) ((sasgd_adamw*)rule)->grad_type = kind;
     Py_BEGIN_ALLOW_THREADS
@@ -538,6 +540,11 @@ static PyObject* apply_adamw(PyObject* self, PyObject* const* a, Py_ssize_t narg
                           (const int64_t*)step_dev, (const float*)factor.data, stream, err, sizeof(err));
     Py_END_ALLOW_THREADS
   }
+  while (held > 0) {
+    held--;
+    Py_DECREF(one[held]);
+  }
+  Py_DECREF(lists);
   PyMem_Free(grads);
   if (failed) return NULL;
   if (rc) return raise_code(rc, err);
