@@ -59,10 +59,30 @@ def build(force=True, verbose=False):
     return LIB
 
 
+# What fastcalls.c uses of torch's C interface to its tensors.
+TENSOR_PROBE = """
+#include <ATen/dlpack.h>
+int usable(const DLPackExchangeAPI* a, void* o, DLTensor* t) {
+  return a->header.version.major == DLPACK_MAJOR_VERSION && a->dltensor_from_py_object_no_sync && a->dltensor_from_py_object_no_sync(o, t) == 0 &&
+         t->device.device_type != kDLCUDA && t->device.device_type != kDLROCM && t->dtype.code == kDLBfloat;
+}
+"""
+
+
+def tensor_flags():
+    """Compiler flags that let the module read tensors through torch's C interface; none where this torch has no such headers, or there is none (it then
+    reads them through their methods)."""
+    spec = importlib.util.find_spec("torch")
+    if spec is None or not spec.origin:
+        return []
+    flags = ["-DSASGD_TORCH_TENSORS", "-I", os.path.join(os.path.dirname(spec.origin), "include")]
+    r = subprocess.run([os.environ.get("CC", "gcc"), "-std=c11", "-fsyntax-only", *flags, "-x", "c", "-"], input=TENSOR_PROBE, capture_output=True, text=True)
+    return flags if r.returncode == 0 else []
+
+
 def build_pyext():
     """The CPython module of the per-gradient and per-update calls (host code only), linked against libsasgd.so beside it."""
-    torch = os.path.join(os.path.dirname(importlib.util.find_spec("torch").origin), "include")
-    cmd = [os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"], "-I", torch, PYEXT_SRC, "-o", PYEXT,
+    cmd = [os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"], *tensor_flags(), PYEXT_SRC, "-o", PYEXT,
            "-L", HERE, "-l:libsasgd.so", "-Wl,-rpath,$ORIGIN"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

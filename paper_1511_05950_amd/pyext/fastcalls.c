@@ -8,7 +8,9 @@
 #include <stdio.h>
 #include <string.h>
 
+#ifdef SASGD_TORCH_TENSORS
 #include <ATen/dlpack.h>               /* torch's tensors through their C interface */
+#endif
 
 #include "../../include/sasgd.h"
 
@@ -275,7 +277,9 @@ typedef struct {
 } view;
 
 static PyObject *tensor_class, *fp32_type, *bf16_type;      /* torch.Tensor, torch.float32, torch.bfloat16: set_tensor_class */
+#ifdef SASGD_TORCH_TENSORS
 static const DLPackExchangeAPI* exchange;                   /* torch's C interface to its tensors, where it has one: 20 ns a tensor instead of 200 */
+#endif
 
 static int bad(PyObject* kind, const char* what, const char* why) {
   PyErr_Format(kind, "%s %s", what, why);
@@ -299,6 +303,7 @@ static int tuple_of(PyObject* o, PyObject* name, int call, int64_t* out, int* di
 
 static int view_of(PyObject* o, view* v) {
   PyObject* a;
+#ifdef SASGD_TORCH_TENSORS
   if (exchange && (PyObject*)Py_TYPE(o) == tensor_class) {
     DLTensor t;
     if (exchange->dltensor_from_py_object_no_sync(o, &t) == 0 && t.ndim <= MOST_DIMS) {
@@ -323,6 +328,7 @@ static int view_of(PyObject* o, view* v) {
     }
     PyErr_Clear();                     /* a kind of tensor that it does not show */
   }
+#endif
   if (address(o, &v->data)) return -1;
   a = PyObject_CallMethodNoArgs(o, s_get_device);
   if (!a) return -1;
@@ -692,7 +698,6 @@ static PyObject* group_norm_gradient(PyObject* self, PyObject* const* a, Py_ssiz
 
 /* set_tensor_class(torch.Tensor, torch.float32, torch.bfloat16) */
 static PyObject* set_tensor_class(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
-  PyObject* capsule;
   NARGS(3);
   Py_INCREF(a[0]);
   Py_INCREF(a[1]);
@@ -700,13 +705,15 @@ static PyObject* set_tensor_class(PyObject* self, PyObject* const* a, Py_ssize_t
   tensor_class = a[0];
   fp32_type = a[1];
   bf16_type = a[2];
-  capsule = PyObject_GetAttrString(a[0], "__dlpack_c_exchange_api__");
+#ifdef SASGD_TORCH_TENSORS
+  PyObject* capsule = PyObject_GetAttrString(a[0], "__dlpack_c_exchange_api__");
   if (capsule) {
     const DLPackExchangeAPI* api = (const DLPackExchangeAPI*)PyCapsule_GetPointer(capsule, "dlpack_exchange_api");
     if (api && api->header.version.major == DLPACK_MAJOR_VERSION && api->dltensor_from_py_object_no_sync) exchange = api;
     Py_DECREF(capsule);
   }
   PyErr_Clear();
+#endif
   Py_RETURN_NONE;
 }
 
