@@ -4,6 +4,7 @@
  * six calls.  Linked against libsasgd.so, which lies next to this module. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <float.h>
 #include <stdint.h>
 #include <stdio.h>
 #include <string.h>
@@ -442,8 +443,10 @@ static PyObject* gradient_norm(PyObject* self, PyObject* const* a, Py_ssize_t na
   if (failed) PyErr_NoMemory();
   else failed = list_of(seq, n, device, &kind, grads, 1, numel, sizeof(int64_t), 0);
   if (!failed) {
+    /* (0 would stand for no bound) */
+    const float bound = max_norm > 0 && (float)max_norm == 0.f ? FLT_TRUE_MIN : (float)max_norm;
     Py_BEGIN_ALLOW_THREADS
-    rc = sasgd_gradientNorm(grads, numel, (int32_t)n, kind == KIND_OTHER ? SASGD_FP32 : kind, (float)max_norm, (float*)out.data, work, stream, err, sizeof(err));
+    rc = sasgd_gradientNorm(grads, numel, (int32_t)n, kind == KIND_OTHER ? SASGD_FP32 : kind, bound, (float*)out.data, work, stream, err, sizeof(err));
     Py_END_ALLOW_THREADS
   }
   Py_DECREF(seq);                     /* (it may be all that holds the gradients: a generator's) */
