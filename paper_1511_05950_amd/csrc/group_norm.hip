@@ -375,9 +375,10 @@ struct HeldMoments {
 };
 // bf16 in units of two channels and more: pairs by the dot product instructions, one instruction a value instead of four.  Distances from 0, so
 // where a lane's values are far from 0 against their spread its squared distances are added up again from its mean.  Sums of kFold vectors in
-// 32 bits, then in 64: a lane's squares are off by less than kFold roundings, and what is left of them after the check by eight times that.
+// 32 bits, of more (LONG) in 64: a lane's squares are off by some kFold roundings, and what is left of them after the check by eight times that.  (The 64-bit
+// sums' registers cost a lane of few vectors: 288 x 54 x 54 x 96 97 us without them, 101 with.)
 constexpr int kFold = 32;
-template <int U>
+template <int U, bool LONG>
 struct DotMoments {
   float s[4], q[4];
   double sum_[U], squares_[U];
@@ -399,7 +400,7 @@ struct DotMoments {
       q[k] = __builtin_amdgcn_fdot2_f32_bf16(x, x, q[k], false);
     }
   }
-  __device__ __forceinline__ void fold() {
+  __device__ __forceinline__ void fold() {         // behind every kFold vectors
 #pragma unroll
     for (int j = 0; j < 4; j++) {
       sum_[j / (4 / U)] += s[j];
@@ -408,20 +409,31 @@ struct DotMoments {
     }
   }
   __device__ __forceinline__ bool close(int count, float (&sum)[U], float (&dev)[U]) {
-    const double inv = count > 0 ? 1.0 / (double)((int64_t)count * (8 / U)) : 0.0;
+    const bool folded = LONG && count > kFold;
+    const float inv = count > 0 ? 1.f / ((float)count * (8 / U)) : 0.f;
     bool fine = true;
-    fold();
+    if (folded) fold();
 #pragma unroll
     for (int k = 0; k < U; k++) {
-      sum[k] = (float)sum_[k];
-      dev[k] = (float)fmax(squares_[k] - sum_[k] * sum_[k] * inv, 0.0);
-      fine = fine && !(dev[k] < 0.125f * (float)squares_[k]);
+      float a = 0.f, b = 0.f;
+#pragma unroll
+      for (int j = k * (4 / U); j < (k + 1) * (4 / U); j++) {
+        a += s[j];
+        b += q[j];
+      }
+      if (folded) {
+        a = (float)sum_[k];
+        b = (float)squares_[k];
+      }
+      sum[k] = a;
+      dev[k] = fmaxf(b - a * a * inv, 0.f);
+      fine = fine && !(dev[k] < 0.125f * b);
     }
     return fine;
   }
 };
-template <typename T, int V, int U, bool HELD> using LaneMoments =
-    std::conditional_t<(V == 8 && U < 8), DotMoments<U>, std::conditional_t<HELD, HeldMoments<T, V, U>, Moments<T, V, U>>>;
+template <typename T, int V, int U, bool HELD, bool LONG> using LaneMoments =
+    std::conditional_t<(V == 8 && U < 8), DotMoments<U, LONG>, std::conditional_t<HELD, HeldMoments<T, V, U>, Moments<T, V, U>>>;
 // Squared distances from the lane's means, once more.
 template <typename T, int V, int U>
 __device__ __forceinline__ void add_distances(const typename Raw<T, V>::type& raw, const float (&mean)[U], float (&dev)[U]) {
@@ -468,17 +480,18 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
     par.put(A, scale + c, scale + S + c);
   }
   {
-    LaneMoments<T, V, U, true> mom;
+    LaneMoments<T, V, U, true, false> mom;
     float sum[U], dev[U];
     mom.start(held[0], count > 0);
 #pragma unroll
     for (int k = 1; k < NV; k++)
       if (k < count) mom.add(held[k]);
+    const float inv = 1.f / ((float)count * (V / U));
     if (!mom.close(count, sum, dev)) {
       float mu[U];
 #pragma unroll
       for (int j = 0; j < U; j++) {
-        mu[j] = sum[j] / (float)(count * (V / U));
+        mu[j] = sum[j] * inv;
         dev[j] = 0.f;
       }
 #pragma unroll
@@ -531,7 +544,7 @@ __global__ __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) void group_nor
 // Images that no workgroup can hold, first launch: the moments of a chunk of positions.  LDS: rows [2 threads U], red [threads], mean and m2 of the units
 constexpr int kAhead = 8;            // loads of a lane on their way (288 x 54 x 54 x 96 forward with 4, 8, 16: 98, 94, 102 us)
 static_assert(kFold % kAhead == 0, "sums are folded between loads");
-template <typename T, int V, int U>
+template <typename T, int V, int U, bool LONG>
 __global__ __launch_bounds__(256) void group_norm_chunk_kernel(const GroupNormArgs A) {
   extern __shared__ float lds[];
   typedef typename Raw<T, V>::type raw_t;
@@ -551,37 +564,38 @@ __global__ __launch_bounds__(256) void group_norm_chunk_kernel(const GroupNormAr
     const int count = count_of(l, np);
     const T* x = x0 + l.row * A.x_pixel + c0 + l.col * V;
     const int64_t step = l.rows * A.x_pixel;
-    LaneMoments<T, V, U, false> mom;
+    LaneMoments<T, V, U, false, LONG> mom;
     float sum[U], dev[U];
     for (int k = 0; k < count || k == 0; k += kAhead) {
       raw_t in[kAhead];
       load_rows<false>(in, x + k * step, step, count - k);
       if (k == 0) mom.start(in[0], count > 0);
-      else if (k % kFold == 0) mom.fold();
+      else if (LONG && k % kFold == 0) mom.fold();
 #pragma unroll
       for (int i = 0; i < kAhead; i++)
         if (k + i < count && k + i > 0) mom.add(in[i]);
     }
     if (!mom.close(count, sum, dev)) {
-      float mu[U], part[U];
+      float mu[U];
       double total[U];
 #pragma unroll
       for (int j = 0; j < U; j++) {
         mu[j] = sum[j] / (float)(count * (V / U));
+        dev[j] = 0.f;
         total[j] = 0.0;
-        part[j] = 0.f;
       }
       for (int k = 0; k < count; k++) {
-        add_distances<T, V, U>(*(const raw_t*)(x + k * step), mu, part);
-        if (k % kFold == kFold - 1 || k == count - 1)
+        add_distances<T, V, U>(*(const raw_t*)(x + k * step), mu, dev);
+        if (LONG && k % kFold == kFold - 1)
 #pragma unroll
           for (int j = 0; j < U; j++) {
-            total[j] += part[j];
-            part[j] = 0.f;
+            total[j] += dev[j];
+            dev[j] = 0.f;
           }
       }
+      if (LONG)
 #pragma unroll
-      for (int j = 0; j < U; j++) dev[j] = (float)total[j];
+        for (int j = 0; j < U; j++) dev[j] = (float)(total[j] + dev[j]);
     }
     unit_moments<V, U>(sum, dev, cols, l, np, rows, red, mean + c0 / (V / U), m2 + c0 / (V / U));
   }
@@ -1223,7 +1237,8 @@ static hipError_t forward(GroupNormArgs& a, hipStream_t stream) {
     }
     return hipGetLastError();
   }
-  group_norm_chunk_kernel<T, V, U><<<grid, a.plan.threads, lds_bytes(a, false), stream>>>(a);
+  if (V == 8 && U < 8 && a.plan.chunk > kFold * a.cols[0].rows) group_norm_chunk_kernel<T, V, U, V == 8 && U < 8><<<grid, a.plan.threads, lds_bytes(a, false), stream>>>(a);
+  else group_norm_chunk_kernel<T, V, U, false><<<grid, a.plan.threads, lds_bytes(a, false), stream>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   auto launch = [&](auto act) { group_norm_apply_kernel<T, V, decltype(act)::value><<<grid, a.plan.threads, (size_t)a.s.groups * (1 + a.spread) * 8, stream>>>(a); };
