@@ -263,7 +263,8 @@ int sasgd_momentElements(const int64_t* numel, int32_t count, int64_t* out_eleme
  *   grads_dev: HOST array of count c device pointers, those of tensor k at [k c .. k c + c); staleness: HOST int32 [c];
  *   step: t >= 1; step_dev: optional device int64 that holds t instead (a captured graph reads it at every replay);
  *   factor_dev: optional device float, gradientNorm's out_dev + 1; where it holds NaN the step is left out: the moments stay, and
- *   theta_out / shadow_out take theta_in.
+ *   theta_out / shadow_out take theta_in.  With c > 1 it multiplies the sum, whose norm no call gives: the factor of one of the gradients does not bound it,
+ *   the least of all c factors does (the shares a_l / sum a are not negative and add up to 1; NaN where one of the factors is NaN).
  * Errors: EINVAL (argument), EHIP. */
 int sasgd_applyAdamW(const sasgd_adamw* rule, const sasgd_tensor* tensors, int32_t count, const void* const* grads_dev, int32_t c,
                      const int32_t* staleness, const sasgd_moments* moments, int64_t step, const int64_t* step_dev,
@@ -271,7 +272,8 @@ int sasgd_applyAdamW(const sasgd_adamw* rule, const sasgd_tensor* tensors, int32
 
 /* useAdamW: from the next applyUpdate on the context's server takes AdamW steps (applyAdamW, on the whole vector as one tensor) instead of the
  * momentum rule; alpha0, lr_mode and weight_decay stay the context's, rule's beta1, beta2, epsilon, seed and kind of moments are read.  The
- * moments, sasgd_momentElements of P, are the caller's, start as zeros and stay in use until the next useAdamW or the context's end;
+ * moments, sasgd_momentElements of P, are the caller's, start as zeros and stay in use until the next useAdamW or the context's end, and until
+ * what the context's stream holds by then has run;
  * the steps count from 1 at the next update.  rule NULL: back to the momentum rule (its momentum is as it was).  Updates are enqueued
  * before applyUpdate returns; gradients that learners hold as factors are written out first (SASGD_FLAG_FLAT_FC_GRADIENT saves that).
  * copyMomentum fails with ESTATE meanwhile.  Errors: EINVAL (rule, moments), ESTATE while a window is closed. */

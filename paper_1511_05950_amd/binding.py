@@ -458,7 +458,7 @@ class AdamW:
     def apply(self, grads, step, staleness=None, scale=None, step_dev=None, stream=None):
         """One step.  grads: c lists of a gradient per tensor, contiguous and of one type, float32 or bfloat16; staleness: one per list
         (0 if not given); step: 1 in the first step (step_dev: a device int64 tensor that holds it instead); scale: device float, the
-        factor of gradientNorm (its out[1:])."""
+        factor of gradientNorm (its out[1:]).  It multiplies the lists' weighted sum, which the least of all lists' factors bounds, and one list's does not."""
         device, stream = _place(stream)
         if step_dev is not None:
             _want("step_dev", step_dev, ("int64",), 1)

@@ -15,10 +15,10 @@
 // left: a lane's squares less its sum's (Moments, DotMoments), good to 32 bits or to 256 roundings of them, and that of an image's at most 64 chunks
 // (group_norm_apply_kernel), of distances from the first one's mean, good to 64 times the few roundings of its sums.
 //
-// What bounds it now (MI355X; a copy of these tensors runs at 4.7 TB/s): bf16 2 304 x 32 x 32 x 32 gradient 105 us, 4.3 TB/s; 288 x 27 x 27 x 256
-// gradient 78 us, 4.1 TB/s: HBM, and the vector ALU between the phases of a workgroup.  288 x 54 x 54 x 96 forward 96 us: 35 of statistics, 59 at the copy's
-// rate; held in slabs of 24 channels it was 106 (segments of 48 bytes of a line).  16 x 64 x 64 x 320 34 us: both launches' ends.  4 x 32 x 32 x 32
-// fp32 7 us: a launch and the chain of its phases.
+// What bounds it now (MI355X; a copy of 160 MB runs at 5.36 TB/s, reading and writing, of 4 GiB at 4.74): bf16 2 304 x 32 x 32 x 32 gradient 104 us, 4.4 TB/s;
+// 288 x 27 x 27 x 256 gradient 77 us, 4.2 TB/s: HBM, and the vector ALU between the phases of a workgroup.  288 x 54 x 54 x 96 forward 97 us (95 to 101 from run
+// to run): 37 of statistics, 60 at the copy's rate; held in slabs of 24 channels by 256 lanes it was 106 (segments of 48 bytes of a line), in larger slabs by more lanes it
+// has not been tried.  16 x 64 x 64 x 320 33 us: the second read, and both launches' ends.  4 x 32 x 32 x 32 fp32 6.5 us: a launch and the chain of its phases.
 #include "dev_common.hpp"
 #include "operators.hpp"
 
@@ -576,6 +576,7 @@ __global__ __launch_bounds__(256) void group_norm_chunk_kernel(const GroupNormAr
         if (k + i < count && k + i > 0) mom.add(in[i]);
     }
     if (!mom.close(count, sum, dev)) {
+      // (read once more: 288 x 54 x 54 x 96 whose channels lie five deviations from 0 114 us instead of 97)
       float mu[U];
       double total[U];
 #pragma unroll
